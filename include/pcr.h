@@ -28,7 +28,7 @@
  *     synchronisation. No C++ exception crosses this interface.
  *   - Supported shapes: bf16 K/V/Q, block_size 16, head_dim 64 or 128,
  *     num_q_heads a multiple of num_kv_heads. Anything else returns
- *     PCR_ERR_UNSUPPORTED.
+ *     PCR_ERR_UNSUPPORTED. (pcr_rope_rows, which touches no pool, takes more head_dims.)
  *   - Empty work (n = 0 pairs, T = 0 tokens, a sequence with s = 0) is a no-op
  *     returning PCR_OK.
  *
@@ -387,6 +387,169 @@ pcr_status pcr_decode_attn_workspace_size(int32_t B, int32_t num_q_heads, int32_
 pcr_status pcr_gather_kv(const pcr_kv_pool *pool, const int32_t *block_tables, int32_t max_blocks,
                          const int32_t *starts, const int32_t *cu_out, int32_t B, int32_t total,
                          void *k_out, void *v_out, void *stream);
+
+/*
+ * pcr_assign_blocks -- block tables and slot list of one step, built on the GPU from
+ * the lengths (the device-side counterpart of pcr_plan's table and slot part: Sec. 5's
+ * paged blocks; nothing is read back to the host, and nothing is copied to the device).
+ * For sequence b with p_b = prefix_lens[b] tokens in the pool and s_b = suffix_lens[b] new
+ * ones, held_b = ceil(p_b/bs) entries of its table row hold blocks already; new blocks
+ * fill the entries up to need_b = ceil((p_b+s_b)/bs), taken from the top of the stack
+ * of free block ids free_blocks[0 .. free_count): with new_b = need_b - held_b and off_b
+ * the sum of new over the sequences before b,
+ *     block_tables[b][held_b + i] = free_blocks[free_count - 1 - (off_b + i)],  i < new_b
+ * and every new token t of b, at position pos = p_b + t, gets
+ *     slot = block_tables[b][pos / bs] * bs + pos % bs
+ * at row cu_suffix[b] + t, where cu_suffix are the prefix sums of s.
+ * Served sequences: b is served when, for it and every sequence before it, the lengths
+ * are not negative, the row has room (need <= max_blocks), and the new blocks and the
+ * new tokens up to it fit (sum of new <= free_count, sum of s <= slots_cap). From the
+ * first sequence that is not, none is: they take no block and have no rows (s counts 0).
+ * Device arrays:
+ *   prefix_lens[B], suffix_lens[B]   read
+ *   free_blocks[free_cap]            read; free_count[1] read, held to [0, free_cap]
+ *   block_tables[B][max_blocks]      only the new entries are written
+ *   slot_mapping[slots_cap]          rows of tokens as above; -1 (which pcr_append_kv and
+ *                                    pcr_rope_append_kv skip) in the rows after the last
+ *                                    token, and for a table entry outside [0, num_blocks)
+ *   positions[slots_cap]             pos of each row's token, 0 after the last; may be NULL
+ *   cu_suffix[B+1]                   written
+ *   context_lens[B]                  p_b + s_b (p_b where not served); may be prefix_lens itself
+ *   free_count_out[1]                free_count less the blocks taken; may be free_count itself
+ *   status[3]                        sequences served, blocks taken, tokens (cu_suffix[B])
+ * Otherwise the arrays must not overlap. num_blocks: blocks of the pool. The call allocates
+ * nothing and may be captured into a graph; with lengths and counts updated in place each
+ * replay is the next step.
+ * Errors: PCR_ERR_UNSUPPORTED for a block_size other than 16, max_blocks or num_blocks from
+ * 2^27 on (token numbers are int32), or B, free_cap or slots_cap beyond 2^30;
+ * PCR_ERR_INVALID_ARG for negative counts, NULL arrays, or max_blocks or num_blocks < 1.
+ * B = 0 is a no-op only when slots_cap = 0 too; otherwise every row is marked as padding.
+ */
+pcr_status pcr_assign_blocks(int32_t B, const int32_t *prefix_lens, const int32_t *suffix_lens,
+                             int32_t *block_tables, int32_t max_blocks, int32_t block_size, int32_t num_blocks,
+                             const int32_t *free_blocks, int32_t free_cap, const int32_t *free_count,
+                             int32_t *slot_mapping, int32_t *positions, int32_t slots_cap, int32_t *cu_suffix,
+                             int32_t *context_lens, int32_t *free_count_out, int32_t *status, void *stream);
+
+/*
+ * pcr_release_blocks -- the reverse: blocks of ended or shortened sequences go back on
+ * the stack of free ids (the pool side of dropping a request, or the rejected tokens of
+ * a speculative step). Sequence b keeps its first keep_lens[b] of lens[b] tokens: its
+ * entries ceil(keep/bs) .. ceil(len/bs) - 1 are handed back (none if keep >= len; a
+ * negative keep counts as 0, a len beyond the row as its end). Blocks that other sequences
+ * share must lie below keep. With N blocks in all, the k-th in order of (sequence, entry)
+ * goes to free_blocks[free_count + N - 1 - k], so releasing what one pcr_assign_blocks call
+ * took restores the stack. If the N ids do not fit (N > free_cap - free_count) nothing
+ * is released.
+ * Device arrays: lens[B], keep_lens[B], block_tables[B][max_blocks] read (entries keep their
+ * values; the row's length says which count); free_blocks[free_cap] written at and above
+ * free_count; free_count[1] read, held to [0, free_cap]; free_count_out[1] written, may be
+ * free_count itself; status[3]: sequences handled (B, or 0 when nothing was released),
+ * blocks released, N (2^31 - 1 if more). No other overlap. An entry outside [0, num_blocks)
+ * is put on the stack as it is; pcr_assign_blocks gives its tokens no slot.
+ * Errors as pcr_assign_blocks. B = 0 writes the count and the status only.
+ */
+pcr_status pcr_release_blocks(int32_t B, const int32_t *lens, const int32_t *keep_lens, const int32_t *block_tables,
+                              int32_t max_blocks, int32_t block_size, int32_t num_blocks, int32_t *free_blocks,
+                              int32_t free_cap, const int32_t *free_count, int32_t *free_count_out, int32_t *status,
+                              void *stream);
+
+/*
+ * Rotary positions with one or several axes (text position; time, height and width of
+ * image and video patches). Pair j of a head is the dims (j, j + rotary_dim/2), or
+ * (2j, 2j + 1) when interleaved; it belongs to axis pair_axis[j] and turns by
+ * angle = positions[pair_axis[j]][t] * inv_freq[j] for token t:
+ *     (x1, x2) -> scale * (x1 cos - x2 sin, x2 cos + x1 sin)
+ * Dims from rotary_dim on are passed through. inv_freq and pair_axis are host arrays, read
+ * during the call only (they travel in the launch's arguments).
+ *   rotary_dim   a positive multiple of 16, at most head_dim (else PCR_ERR_UNSUPPORTED)
+ *   num_axes     1 to 4
+ *   scale        finite (1 for a pure rotation)
+ * Numerics: the angle is reduced in fp64 (error about |angle| * 2^-52, so positions over
+ * the whole int32 range keep their phase), cos and sin are fp32, the products fp32, one
+ * rounding to bf16 (nearest even) at the end.
+ */
+typedef struct pcr_rope {
+    const float *inv_freq;      /* host [rotary_dim / 2], finite */
+    const int32_t *pair_axis;   /* host [rotary_dim / 2], each 0 .. num_axes - 1; NULL: all 0 */
+    int32_t rotary_dim;
+    int32_t num_axes;
+    int32_t interleaved;        /* 0: pairs (j, j + rotary_dim/2); 1: pairs (2j, 2j + 1) */
+    float scale;
+} pcr_rope;
+
+/*
+ * pcr_rope_append_kv -- rotates the new tokens' Q and K and writes K and V into the pool:
+ * the position encoding that the attention entry points expect of their inputs (cached K
+ * is position-encoded, Sec. 2.2 and 4.2) and pcr_append_kv in one pass over the data.
+ *   q, k_new, v_new  device bf16, token t's heads contiguous at t * stride elements:
+ *                    [Hq][d], [Hkv][d], [Hkv][d] (so the three may be parts of one fused
+ *                    projection's rows); 16-byte aligned, strides multiples of 8 and at
+ *                    least the heads' size
+ *   positions        device int32 [num_axes][T], axis a at a * pos_stride (>= T) elements
+ *   slot_mapping     device int32 [T], as pcr_append_kv: a token whose slot is negative or
+ *                    outside the pool has no K/V written (its Q row is rotated all the same)
+ *   q_out            device bf16 [T][Hq][d] contiguous, 16-byte aligned; may be q itself
+ *                    when q_stride is Hq * d, otherwise the two must not overlap
+ *   num_q_heads      0: no Q (q and q_out are not read)
+ * k_new and v_new must not overlap q_out or the pool. Errors: as pcr_append_kv;
+ * PCR_ERR_INVALID_ARG for the stride, alignment, overlap and rope conditions above.
+ */
+pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, const void *q, int64_t q_stride,
+                              const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                              const int32_t *positions, int64_t pos_stride, const int32_t *slot_mapping, int32_t T,
+                              int32_t num_q_heads, void *q_out, void *stream);
+
+/*
+ * pcr_rope_rows -- the same rotation of plain rows: x [T][num_heads][head_dim] bf16 at
+ * x_stride elements per token, out likewise at out_stride (an encoder's heads, or Q and K
+ * that go to no pool). inverse != 0 applies the transposed map (sin negated): the gradient
+ * with respect to x of a gradient with respect to out, and with scale 1 the undoing.
+ *   head_dim  a multiple of 16 up to 256 (else PCR_ERR_UNSUPPORTED)
+ * out may be x itself when the strides are equal, otherwise they must not overlap; both
+ * 16-byte aligned, strides multiples of 8 and at least num_heads * head_dim. T = 0 is a no-op.
+ */
+pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, const int32_t *positions,
+                         int64_t pos_stride, int32_t T, int32_t num_heads, int32_t head_dim, int32_t inverse,
+                         void *out, int64_t out_stride, void *stream);
+
+/*
+ * pcr_cross_attn -- cross attention: every query row of sequence b attends all n_b =
+ * key_lens[b] states of an encoder (of a length of their own), whose K/V lie in the pool
+ * like any other tokens (written once by pcr_append_kv or loaded from the host store, then
+ * read by every later step). For row t of [cu_q[b], cu_q[b+1]), head h, keys j in [0, n_b):
+ *     out = sum_j softmax_j(sm_scale * <q, k_j>) v_j;   n_b = 0: the rows are zeros
+ * No causal bound and no position encoding. Several row runs over one set of states (beams,
+ * samples) are rows of one sequence; text that sees different images in different parts is
+ * one sequence per part, their table rows naming the images' blocks (blocks may be shared).
+ *   q, out           device bf16 [cu_q[B]][Hq][d], 16-byte aligned, not overlapping; fp32
+ *                    accumulation, rounded to nearest even. Rows from cu_q[B] on are left.
+ *   block_tables     device int32 [B][max_blocks]; entries past ceil(n_b/bs) are not read;
+ *                    an id outside the pool reads block 0
+ *   key_lens[B], cu_q[B+1]   device int32, and host copies of the same (they size the launch
+ *                    and must be equal)
+ *   workspace        device memory owned by the caller, 16-byte aligned, of
+ *                    pcr_cross_attn_workspace_size bytes (NULL when that is 0); scratch. One
+ *                    workspace serves every call ordered on one stream; calls that may
+ *                    overlap (captured graphs that may run together among them) need their own.
+ * Numerics as for pcr_prefix_prefill_attn; slots past n_b are never read into the result.
+ * The split of the work follows from the host lengths and the workspace size alone, so
+ * repeated calls give identical bits.
+ * Errors: as pcr_prefix_prefill_attn, and PCR_ERR_INVALID_ARG when q and out overlap or the
+ * workspace is missing, misaligned or too small (the message names the size needed).
+ */
+pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t *block_tables, int32_t max_blocks,
+                          const int32_t *key_lens, const int32_t *cu_q, const int32_t *host_key_lens,
+                          const int32_t *host_cu_q, int32_t B, int32_t num_q_heads, float sm_scale, void *out,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * pcr_cross_attn_workspace_size -- bytes of workspace that serve every pcr_cross_attn call on
+ * the current device of at most B sequences with at most total_rows query rows in all and at
+ * most max_keys keys each. PCR_ERR_HIP when no device is usable.
+ */
+pcr_status pcr_cross_attn_workspace_size(int32_t B, int32_t total_rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                         int32_t head_dim, int32_t max_keys, int64_t *bytes);
 
 /* Per-layer device inputs and outputs for pcr_pipeline_run. */
 typedef struct pcr_layer_io {

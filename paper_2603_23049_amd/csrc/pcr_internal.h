@@ -14,6 +14,10 @@ constexpr int kBlockSize = 16;   // tokens per pool block (the serving engine's 
 pcr_status fail(pcr_status st, const char *fmt, ...);
 // Turns a HIP error into PCR_ERR_HIP with the call site named.
 pcr_status hip_fail(hipError_t e, const char *what);
+void clear_error();
+// The checks every entry point makes of a block layout and of a pool (errors name `who`).
+pcr_status check_layout(int32_t block_size, int32_t num_kv_heads, int32_t head_dim, const char *who);
+pcr_status check_pool(const pcr_kv_pool *pool, const char *who);
 
 // Up to this many (src, dst) block pairs travel in one pull-kernel launch as
 // kernel arguments (so no device copy of the host lists is needed).

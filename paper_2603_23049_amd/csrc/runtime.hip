@@ -32,9 +32,7 @@ pcr_status hip_fail(hipError_t e, const char *what)
     return fail(PCR_ERR_HIP, "%s: %s (%d)", what, hipGetErrorString(e), (int)e);
 }
 
-namespace {
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+void clear_error() { g_err[0] = 0; }
 
 pcr_status check_layout(int32_t block_size, int32_t num_kv_heads, int32_t head_dim, const char *who)
 {
@@ -58,6 +56,10 @@ pcr_status check_pool(const pcr_kv_pool *pool, const char *who)
         return fail(PCR_ERR_INVALID_ARG, "%s: pool k/v must be 16-byte aligned", who);
     return PCR_OK;
 }
+
+namespace {
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int64_t block_bytes(int32_t block_size, int32_t Hkv, int32_t d) { return kv_block_bytes(block_size, Hkv, d); }
 

@@ -38,6 +38,8 @@ EXPORTS = ["pcr_plan", "pcr_plan_offload", "pcr_load_kv_layer", "pcr_load_kv_lay
            "pcr_offload_kv_layer", "pcr_offload_kv_layer_method", "pcr_offload_kv_layer_staged",
            "pcr_load_kv_layer_staged", "pcr_append_kv",
            "pcr_prefix_prefill_attn", "pcr_prefill_attn_set_schedule", "pcr_prefill_attn_hold_scratch", "pcr_decode_attn", "pcr_decode_attn_noalloc", "pcr_decode_attn_workspace_size", "pcr_gather_kv", "pcr_pipeline_run", "pcr_pipeline_run_staged",
+           "pcr_assign_blocks", "pcr_release_blocks", "pcr_rope_append_kv", "pcr_rope_rows", "pcr_cross_attn",
+           "pcr_cross_attn_workspace_size",
            "pcr_pipeline_run_offload", "pcr_pipeline_run_offload_staged",
            "pcr_store_open", "pcr_store_write_async", "pcr_store_read_async", "pcr_store_wait",
            "pcr_store_poll", "pcr_store_stats", "pcr_store_close", "pcr_last_error", "pcr_version"]
@@ -59,6 +61,11 @@ class _Host(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("num_blocks", ctypes.c_int64),
                 ("block_size", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("pair_axis", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32),
+                ("num_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class _LayerIO(ctypes.Structure):
@@ -100,6 +107,13 @@ def lib():
                                               P]
         L.pcr_decode_attn_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_int64)]
         L.pcr_gather_kv.argtypes = [ctypes.POINTER(_Pool), P, i32, P, P, i32, i32, P, P, P]
+        L.pcr_assign_blocks.argtypes = [i32, P, P, P, i32, i32, i32, P, i32, P, P, P, i32, P, P, P, P, P]
+        L.pcr_release_blocks.argtypes = [i32, P, P, P, i32, i32, i32, P, i32, P, P, P, P]
+        L.pcr_rope_append_kv.argtypes = [P, ctypes.POINTER(_Pool), P, i64, P, i64, P, i64, P, i64, P, i32, i32, P, P]
+        L.pcr_rope_rows.argtypes = [P, P, i64, P, i64, i32, i32, i32, i32, P, i64, P]
+        L.pcr_cross_attn.argtypes = [P, ctypes.POINTER(_Pool), P, i32, P, P, P, P, i32, i32, ctypes.c_float, P, P,
+                                     i64, P]
+        L.pcr_cross_attn_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
         L.pcr_pipeline_run.argtypes = [ctypes.POINTER(_LayerIO), i32, ctypes.POINTER(_Batch), ctypes.c_int, P, P,
                                        P]
         L.pcr_pipeline_run_staged.argtypes = [ctypes.POINTER(_LayerIO), i32, ctypes.POINTER(_Batch), P, i64, P, P,
@@ -434,6 +448,201 @@ def gather_kv(pool: KVPool, block_tables, starts, cu_out, total: int, k_out, v_o
     p = pool.c()
     _check(lib().pcr_gather_kv(ctypes.byref(p), _ptr(block_tables), int(block_tables.shape[1]), _ptr(starts),
                                _ptr(cu_out), B, int(total), _ptr(k_out), _ptr(v_out), _stream(stream)))
+
+
+def _current_gpu():
+    """(torch, the current GPU's index; -2 on a machine without one, which no tensor has)."""
+    import torch
+    return torch, torch._C._cuda_getDevice() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2
+
+
+def _refuse(x, n: int, dtype: str, cur: int, what: str):
+    """Says which of the conditions of a device array does not hold."""
+    if str(x.dtype) != dtype and not (dtype == "2-byte" and x.element_size() == 2):
+        raise ValueError(f"{what} holds {x.dtype}, not {dtype} elements")
+    if x.numel() < n:
+        raise ValueError(f"{what} holds {x.numel()} elements, the call takes {n}")
+    if x.get_device() != cur:
+        raise ValueError(f"{what} is on {x.device}, not on the current GPU")
+    raise ValueError(f"{what} is not contiguous")
+
+
+def _ints(gpu, n: int, x, what: str):
+    """The address of an int32 array of at least n elements on the current GPU."""
+    if x.dtype is not gpu[0].int32 or x.numel() < n or x.get_device() != gpu[1] or not x.is_contiguous():
+        _refuse(x, n, "torch.int32", gpu[1], what)
+    return x.data_ptr()
+
+
+def _halves(gpu, n: int, x, what: str):
+    """The same of 2-byte elements."""
+    if x.element_size() != 2 or x.numel() < n or x.get_device() != gpu[1] or not x.is_contiguous():
+        _refuse(x, n, "2-byte", gpu[1], what)
+    return x.data_ptr()
+
+
+def _pool_here(gpu, pool: KVPool):
+    """The pool's handle, once its arrays are found to be as long as the library takes them to be."""
+    n = pool.num_blocks * pool.num_kv_heads * pool.block_size * pool.head_dim
+    _halves(gpu, n, pool.k, "pool.k")
+    _halves(gpu, n, pool.v, "pool.v")
+    return pool.c()
+
+
+def assign_blocks(prefix_lens, suffix_lens, block_tables, free_blocks, free_count, num_blocks: int, slot_mapping,
+                  cu_suffix, context_lens, free_count_out, status, positions=None, block_size: int = 16, stream=None):
+    """pcr_assign_blocks: all arrays int32 device tensors. prefix_lens, suffix_lens and
+    context_lens [B], block_tables [B][max_blocks], free_blocks [free_cap], free_count and
+    free_count_out [1], slot_mapping (and positions) [slots_cap], cu_suffix [B+1], status [3].
+    context_lens may be prefix_lens, free_count_out may be free_count."""
+    B, cap = prefix_lens.shape[0], slot_mapping.shape[0]
+    if block_tables.dim() != 2:
+        raise ValueError("block_tables must be [B][max_blocks]")
+    mb, gpu = block_tables.shape[1], _current_gpu()
+    _check(lib().pcr_assign_blocks(
+        B, _ints(gpu, B, prefix_lens, "prefix_lens"), _ints(gpu, B, suffix_lens, "suffix_lens"),
+        _ints(gpu, B * mb, block_tables, "block_tables"), mb, block_size, num_blocks,
+        _ints(gpu, 0, free_blocks, "free_blocks"), free_blocks.numel(), _ints(gpu, 1, free_count, "free_count"),
+        _ints(gpu, cap, slot_mapping, "slot_mapping"),
+        None if positions is None else _ints(gpu, cap, positions, "positions"), cap,
+        _ints(gpu, B + 1, cu_suffix, "cu_suffix"), _ints(gpu, B, context_lens, "context_lens"),
+        _ints(gpu, 1, free_count_out, "free_count_out"), _ints(gpu, 3, status, "status"), _stream(stream)))
+
+
+def release_blocks(lens, keep_lens, block_tables, free_blocks, free_count, num_blocks: int, free_count_out, status,
+                   block_size: int = 16, stream=None):
+    """pcr_release_blocks: int32 device tensors, shaped as for assign_blocks."""
+    B = lens.shape[0]
+    if block_tables.dim() != 2:
+        raise ValueError("block_tables must be [B][max_blocks]")
+    mb, gpu = block_tables.shape[1], _current_gpu()
+    _check(lib().pcr_release_blocks(
+        B, _ints(gpu, B, lens, "lens"), _ints(gpu, B, keep_lens, "keep_lens"),
+        _ints(gpu, B * mb, block_tables, "block_tables"), mb, block_size, num_blocks,
+        _ints(gpu, 0, free_blocks, "free_blocks"), free_blocks.numel(), _ints(gpu, 1, free_count, "free_count"),
+        _ints(gpu, 1, free_count_out, "free_count_out"), _ints(gpu, 3, status, "status"), _stream(stream)))
+
+
+class Rope:
+    """A rotation (pcr_rope): inv_freq [rotary_dim/2] and pair_axis [rotary_dim/2] (or None) are
+    host arrays, copied here."""
+
+    def __init__(self, inv_freq, pair_axis=None, num_axes: int = 1, interleaved: bool = False, scale: float = 1.0):
+        self.inv_freq = np.array(inv_freq, dtype=np.float32).reshape(-1)
+        self.pair_axis = None if pair_axis is None else np.array(pair_axis, dtype=np.int32).reshape(-1)
+        if self.pair_axis is not None and self.pair_axis.size != self.inv_freq.size:
+            raise ValueError("inv_freq and pair_axis differ in length")
+        self.num_axes = int(num_axes)
+        self._c = _Rope(self.inv_freq.ctypes.data, None if self.pair_axis is None else self.pair_axis.ctypes.data,
+                        2 * self.inv_freq.size, self.num_axes, int(bool(interleaved)), float(scale))
+        self._addr = ctypes.addressof(self._c)
+
+
+def _positions(gpu, positions, num_axes: int, T: int) -> int:
+    """Checks positions [num_axes][T] (or [T] with one axis), an axis's back to back; returns
+    the elements from one axis to the next."""
+    if positions.dtype is not gpu[0].int32:
+        raise ValueError(f"positions hold {positions.dtype}, not torch.int32")
+    shape, st = tuple(positions.shape), positions.stride()
+    if shape != (num_axes, T) and not (num_axes == 1 and shape == (T,)):
+        raise ValueError(f"positions must be [{num_axes}][{T}], not {list(shape)}")
+    if T > 1 and st[-1] != 1:
+        raise ValueError("positions of one axis are not back to back")
+    if num_axes > 1 and st[0] < T:
+        raise ValueError("positions of two axes overlap")
+    if positions.get_device() != gpu[1]:
+        raise ValueError(f"positions are on {positions.device}, not on the current GPU")
+    return st[0] if num_axes > 1 else T
+
+
+def _rows(gpu, x, T: int, H: int, d: int, what: str) -> int:
+    """Checks x [T][H][d] (or [T][H*d]) of 2-byte elements, a token's heads back to back;
+    returns the elements from one token to the next."""
+    shape, st = tuple(x.shape), x.stride()
+    if shape != (T, H, d) and shape != (T, H * d):
+        raise ValueError(f"{what} must be [{T}][{H}][{d}], not {list(shape)}")
+    if x.element_size() != 2:
+        raise ValueError(f"{what} holds {x.dtype}, not 2-byte elements")
+    if T > 0 and (st[-1] != 1 or (len(shape) == 3 and H > 1 and st[1] != d)):
+        raise ValueError(f"{what}: the heads of a token are not back to back")
+    if x.get_device() != gpu[1]:
+        raise ValueError(f"{what} is on {x.device}, not on the current GPU")
+    return st[0] if T > 1 else H * d
+
+
+def rope_append_kv(rope: Rope, pool: KVPool, q, k_new, v_new, positions, slot_mapping, num_q_heads: int, q_out,
+                   stream=None):
+    """pcr_rope_append_kv: q [T][Hq][d], k_new and v_new [T][Hkv][d] with any token stride (parts
+    of a fused projection's rows, for instance), positions [num_axes][T], slot_mapping [T];
+    q_out [T][Hq][d] contiguous, may be q. q and q_out None with num_q_heads 0: K and V only."""
+    T, Hkv, d, Hq, gpu = k_new.shape[0], pool.num_kv_heads, pool.head_dim, num_q_heads, _current_gpu()
+    ks, vs = _rows(gpu, k_new, T, Hkv, d, "k_new"), _rows(gpu, v_new, T, Hkv, d, "v_new")
+    qs, qp, op = 0, None, None
+    if Hq > 0:
+        qs, qp = _rows(gpu, q, T, Hq, d, "q"), q.data_ptr()
+        op = _halves(gpu, T * Hq * d, q_out, "q_out")
+    ps = _positions(gpu, positions, rope.num_axes, T)
+    sp = _ints(gpu, T, slot_mapping, "slot_mapping")
+    p = _pool_here(gpu, pool)
+    _check(lib().pcr_rope_append_kv(rope._addr, ctypes.byref(p), qp, qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs,
+                                    positions.data_ptr(), ps, sp, T, Hq, op, _stream(stream)))
+
+
+def rope_rows(rope: Rope, x, positions, out, inverse: bool = False, stream=None):
+    """pcr_rope_rows: x and out [T][H][d] with any token stride (out may be x), positions
+    [num_axes][T]. inverse: the transposed map (the gradient; with scale 1 the undoing)."""
+    (T, H, d), gpu = x.shape, _current_gpu()
+    xs, os_ = _rows(gpu, x, T, H, d, "x"), _rows(gpu, out, T, H, d, "out")
+    ps = _positions(gpu, positions, rope.num_axes, T)
+    _check(lib().pcr_rope_rows(rope._addr, x.data_ptr(), xs, positions.data_ptr(), ps, T, H, d, int(bool(inverse)),
+                               out.data_ptr(), os_, _stream(stream)))
+
+
+def cross_attn_workspace_bytes(B: int, total_rows: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
+                               max_keys: int) -> int:
+    """pcr_cross_attn_workspace_size on the current device."""
+    n = ctypes.c_int64(0)
+    _check(lib().pcr_cross_attn_workspace_size(int(B), int(total_rows), int(num_q_heads), int(num_kv_heads),
+                                               int(head_dim), int(max_keys), ctypes.byref(n)))
+    return int(n.value)
+
+
+def cross_attn(q, pool: KVPool, block_tables, key_lens, cu_q, host_key_lens, host_cu_q, num_q_heads: int, out,
+               workspace=None, sm_scale: Optional[float] = None, stream=None):
+    """pcr_cross_attn. q/out [T][Hq][d], block_tables [B][max_blocks], key_lens [B], cu_q [B+1] on
+    the device; host_* are the host copies of the lengths. Without a workspace one of the
+    needed size is allocated as decode_attn does."""
+    hkl, hcu = _i32_host(host_key_lens), _i32_host(host_cu_q)
+    B, d, Hq = int(hkl.shape[0]), pool.head_dim, int(num_q_heads)
+    if hcu.shape[0] != B + 1:
+        raise ValueError("host_cu_q must have B+1 entries")
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    T, mb, gpu = int(hcu[-1]), block_tables.shape[1], _current_gpu()
+    qp, op = _halves(gpu, T * Hq * d, q, "q"), _halves(gpu, T * Hq * d, out, "out")
+    btp = _ints(gpu, B * mb, block_tables, "block_tables")
+    klp, cup = _ints(gpu, B, key_lens, "key_lens"), _ints(gpu, B + 1, cu_q, "cu_q")
+    p = _pool_here(gpu, pool)
+    if workspace is None and T > 0:
+        n = cross_attn_workspace_bytes(B, T, Hq, pool.num_kv_heads, d, int(hkl.max()))
+        if n > 0:
+            import torch
+            if stream is None:
+                s = torch.cuda.current_stream(q.device)
+            elif isinstance(stream, int):
+                s = torch.cuda.ExternalStream(stream, device=q.device)
+            else:
+                s = stream
+            with torch.cuda.stream(s):
+                workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+    wsp, ws_bytes = None, 0
+    if workspace is not None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+        if workspace.get_device() != gpu[1] or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous and on the current GPU")
+        wsp = workspace.data_ptr()
+    _check(lib().pcr_cross_attn(qp, ctypes.byref(p), btp, mb, klp, cup, _ptr(hkl), _ptr(hcu), B, Hq, sm_scale, op, wsp,
+                                ws_bytes, _stream(stream)))
 
 
 @dataclass

@@ -1,0 +1,217 @@
+"""GPU: rotary positions against the rotation in 64 bits, on plain rows (forward, transposed)
+and fused with the write into the pool. Values are bf16, angles far beyond fp32's phase.
+
+Tolerance: the products and sums are fp32 and cos and sin are off by at most 2^-21 together
+with the angle (its fp32 rest 2^-23.4, the fp64 product |angle| 2^-52 <= 2^-21 for the angles
+below 2^31 here), so a result is off by 2^-19 (|x1| + |x2|) * scale with room, and half a bf16
+step, 2^-8 of the value, from the one rounding."""
+import numpy as np
+import pytest
+import torch
+
+import opref
+from paper_2603_23049_amd import pcr
+
+pytestmark = pytest.mark.gpu
+BS = 16
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _bf16(gen, *shape):
+    return torch.randn(shape, generator=gen).to(torch.bfloat16)
+
+
+def _rotation(rd, axes, seed=0):
+    rng = np.random.Generator(np.random.PCG64(seed))
+    f = (10000.0 ** (-np.arange(rd // 2) / (rd // 2))).astype(np.float32)
+    axis = np.arange(rd // 2) % axes if seed % 2 else np.sort(rng.integers(0, axes, size=rd // 2))
+    return f, axis.astype(np.int32)
+
+
+def _positions(gen, axes, T, far):
+    pos = torch.randint(-far if far < 2 ** 20 else 0, far, (axes, T), generator=gen, dtype=torch.int64)
+    if T > 2:
+        pos[:, 0], pos[:, 1], pos[:, 2] = 0, far - 1, 1
+    return pos.to(torch.int32)
+
+
+def _close(got, x, pos, f, axis, interleaved, scale=1.0, inverse=False):
+    want, size = opref.rotate(x.double(), pos, f, axis, interleaved, scale, inverse)
+    err = (got.cpu().double() - want).abs()
+    tol = want.abs() * 2.0 ** -8 + size * scale * 2.0 ** -19
+    assert torch.isfinite(got.float()).all() and (err <= tol).all(), float((err - tol).max())
+
+
+@pytest.mark.parametrize("T,H,d,rd,axes,interleaved,far", [
+    (1, 1, 16, 16, 1, 0, 100), (1, 8, 64, 64, 1, 0, 2 ** 31 - 1), (3, 5, 80, 80, 2, 0, 128), (67, 16, 80, 48, 3, 1, 4096),
+    (130, 3, 128, 128, 3, 0, 10 ** 6), (33, 40, 128, 64, 4, 1, 2 ** 31 - 1), (19, 2, 256, 256, 1, 1, 10 ** 7),
+    (5, 7, 192, 16, 2, 0, 50), (257, 1, 48, 32, 1, 0, 2 ** 20), (1000, 6, 96, 96, 3, 1, 2 ** 24), (7, 1, 240, 240, 4, 0, 9)])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rows(T, H, d, rd, axes, interleaved, far, inverse):
+    gen = _gen(T * 100 + d)
+    x, pos = _bf16(gen, T, H, d), _positions(gen, axes, T, far)
+    f, axis = _rotation(rd, axes, T)
+    rope = pcr.Rope(f, axis, axes, bool(interleaved))
+    xd, pd = x.cuda(), pos.cuda()
+    out = torch.full((T + 2, H, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    pcr.rope_rows(rope, xd, pd, out[1:T + 1], inverse=inverse)
+    _close(out[1:T + 1], x, pos, f, axis, interleaved, inverse=inverse)
+    assert (out[0] == 7).all() and (out[T + 1] == 7).all()
+    assert torch.equal(xd.cpu(), x)
+    # dims past the rotation keep their bits; in place gives the same bits
+    assert torch.equal(out[1:T + 1, :, rd:].cpu(), x[:, :, rd:])
+    pcr.rope_rows(rope, xd, pd, xd, inverse=inverse)
+    assert torch.equal(xd, out[1:T + 1])
+
+
+def test_rows_strided_scaled_and_one_axis_default():
+    gen = _gen(5)
+    T, H, d = 70, 6, 64
+    wide = _bf16(gen, T, 3 * H * d + 8)
+    x = wide[:, 8:8 + H * d].unflatten(1, (H, d))
+    pos = _positions(gen, 1, T, 5000)
+    f, _ = _rotation(32, 1)
+    wd = wide.cuda()
+    xd = wd[:, 8:8 + H * d].unflatten(1, (H, d))
+    od = torch.zeros(T, 2 * H * d, dtype=torch.bfloat16, device="cuda")
+    pcr.rope_rows(pcr.Rope(f, scale=1.25), xd, pos.cuda()[0], od[:, H * d:].unflatten(1, (H, d)))
+    _close(od[:, H * d:].unflatten(1, (H, d)), x, pos, f, np.zeros(16, int), 0, scale=1.25)
+    assert (od[:, :H * d] == 0).all()
+    pcr.rope_rows(pcr.Rope(f), xd, pos.cuda(), xd)          # in place inside the wide rows
+    _close(xd, x, pos, f, np.zeros(16, int), 0)
+    same = torch.ones(3 * H * d + 8, dtype=torch.bool)
+    same[8:8 + H * d] = False
+    assert torch.equal(wd.cpu()[:, same], wide[:, same])
+
+
+def test_rows_gradient_is_the_transpose():
+    """<rope(x), g> = <x, rope_inverse(g)> and, in fp32 rotations of the same kernel's inputs,
+    differences along x: the map is linear, so a difference is the map of the difference."""
+    gen = _gen(9)
+    T, H, d = 40, 3, 64
+    x, g = _bf16(gen, T, H, d), _bf16(gen, T, H, d)
+    pos = _positions(gen, 2, T, 3000)
+    f, axis = _rotation(64, 2)
+    rope = pcr.Rope(f, axis, 2)
+    gx = torch.empty(T, H, d, dtype=torch.bfloat16, device="cuda")
+    pcr.rope_rows(rope, g.cuda(), pos.cuda(), gx, inverse=True)
+    # against differences of the 64-bit rotation's product with g, one coordinate at a time
+    for t, h, e in ((0, 0, 0), (1, 2, 33), (17, 1, 63), (39, 0, 31)):
+        step = torch.zeros(T, H, d, dtype=torch.float64)
+        step[t, h, e] = 0.5
+        up, _ = opref.rotate(x.double() + step, pos, f, axis, 0)
+        dn, _ = opref.rotate(x.double() - step, pos, f, axis, 0)
+        slope = float(((up - dn) * g.double()).sum())
+        pair = float(g[t, h].abs().max())
+        assert abs(float(gx[t, h, e]) - slope) <= abs(slope) * 2.0 ** -8 + 2 * pair * 2.0 ** -19
+    # undoing: two roundings of at most half a step each of values up to |x1| + |x2|
+    y = torch.empty_like(gx)
+    pcr.rope_rows(rope, x.cuda(), pos.cuda(), y)
+    pcr.rope_rows(rope, y, pos.cuda(), y, inverse=True)
+    _, size = opref.rotate(x.double(), pos, f, axis, 0)
+    assert ((y.cpu().double() - x.double()).abs() <= size * (2.0 ** -8 * 2.5)).all()
+
+
+def _append_case(T, Hq, Hkv, d, rd, axes, interleaved, fused, far, seed, bad=()):
+    gen = _gen(seed)
+    rng = np.random.Generator(np.random.PCG64(seed))
+    slots, blocks = [], 0
+    while len(slots) < T:                                  # runs that start and end inside blocks
+        a, n = int(rng.integers(0, 40)), int(rng.integers(1, 60))
+        slots += [(blocks * BS + a + i) for i in range(min(n, T - len(slots)))]
+        blocks += -(-(a + n) // BS)
+    nb = blocks + 3
+    perm = rng.permutation(nb)
+    slots = np.array([perm[s // BS] * BS + s % BS for s in slots], np.int64)
+    for i in bad:
+        slots[i % T] = (-1, nb * BS, 2 ** 31 - 1, -2 ** 31)[i % 4]
+    if fused:
+        qkv = _bf16(gen, T, (Hq + 2 * Hkv) * d)
+        q, k, v = (t.unflatten(1, (-1, d)) for t in qkv.split([Hq * d, Hkv * d, Hkv * d], dim=1))
+        qkvd = qkv.cuda()
+        qd, kd, vd = (t.unflatten(1, (-1, d)) for t in qkvd.split([Hq * d, Hkv * d, Hkv * d], dim=1))
+    else:
+        q, k, v = _bf16(gen, T, Hq, d), _bf16(gen, T, Hkv, d), _bf16(gen, T, Hkv, d)
+        qd, kd, vd = q.cuda(), k.cuda(), v.cuda()
+    pk, pv = _bf16(gen, nb, Hkv, BS * d), _bf16(gen, nb, Hkv, BS * d)
+    pos = _positions(gen, axes, T, far)
+    f, axis = _rotation(rd, axes, seed)
+    return dict(q=q, k=k, v=v, qd=qd, kd=kd, vd=vd, pk=pk, pv=pv, pos=pos, f=f, axis=axis, slots=slots, nb=nb,
+                rope=pcr.Rope(f, axis, axes, bool(interleaved)))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d,rd,axes,interleaved,fused,far,bad", [
+    (1, 8, 8, 64, 64, 1, 0, 0, 100, ()), (1, 4, 1, 128, 128, 3, 0, 1, 2 ** 31 - 1, ()), (2, 1, 1, 64, 16, 1, 1, 1, 10, ()),
+    (17, 6, 3, 64, 32, 2, 0, 0, 4096, (0, 5)), (64, 32, 8, 128, 128, 3, 0, 1, 100000, (3,)),
+    (333, 16, 2, 128, 64, 1, 1, 0, 10 ** 6, (0, 1, 2, 3, 100, 331)), (201, 28, 4, 128, 128, 3, 1, 1, 2 ** 20, ()),
+    (700, 8, 1, 64, 64, 4, 0, 1, 5000, (9,)), (95, 64, 8, 128, 32, 2, 0, 0, 77, ()), (4100, 2, 2, 64, 64, 1, 0, 1, 9999, ()),
+    (2500, 8, 8, 128, 128, 3, 0, 1, 33000, (2499, 7, 64)), (31, 0, 3, 64, 48, 1, 0, 0, 100, (1,))])
+def test_append(T, Hq, Hkv, d, rd, axes, interleaved, fused, far, bad):
+    c = _append_case(T, Hq, Hkv, d, rd, axes, interleaved, fused, far, T + d, bad)
+    pool = pcr.KVPool(c["pk"].cuda(), c["pv"].cuda(), Hkv, d)
+    out = torch.full((T + 1, Hq, d), 3.0, dtype=torch.bfloat16, device="cuda")
+    pcr.rope_append_kv(c["rope"], pool, c["qd"] if Hq else None, c["kd"], c["vd"], c["pos"].cuda(),
+                       torch.from_numpy(c["slots"].astype(np.int32)).cuda(), Hq, out[:T] if Hq else None)
+    torch.cuda.synchronize()
+    if Hq:
+        _close(out[:T], c["q"], c["pos"], c["f"], c["axis"], interleaved)
+        assert (out[T] == 3).all()
+    # the pool: rotated K, V bit for bit, every other slot as it was
+    live = (c["slots"] >= 0) & (c["slots"] < c["nb"] * BS)
+    blk, o = torch.from_numpy(c["slots"][live] // BS), torch.from_numpy(c["slots"][live] % BS)
+    k_got = pool.k.cpu().view(c["nb"], Hkv, BS, d)
+    _close(k_got[blk, :, o], c["k"][live], c["pos"][:, live], c["f"], c["axis"], interleaved)
+    want_v = c["pv"].clone().view(c["nb"], Hkv, d, BS)
+    want_v[blk, :, :, o] = c["v"][live]
+    assert torch.equal(pool.v.cpu().view(torch.int16), want_v.view(c["nb"], Hkv, BS * d).view(torch.int16))
+    rest = torch.ones(c["nb"], BS, dtype=torch.bool)
+    rest[blk, o] = False
+    old = c["pk"].view(c["nb"], Hkv, BS, d).permute(0, 2, 1, 3)[rest]
+    assert torch.equal(k_got.permute(0, 2, 1, 3)[rest].contiguous().view(torch.int16), old.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(5, 8, 2, 64), (1200, 32, 8, 128)])
+def test_append_equals_rows_then_append(T, Hq, Hkv, d):
+    """The fused call's bits are those of the rotation of plain rows and pcr_append_kv; in
+    place over Q too, on a stream of its own, and again from a captured graph."""
+    c = _append_case(T, Hq, Hkv, d, d, 3, 0, 0, 70000, 3)
+    posd, slots = c["pos"].cuda(), torch.from_numpy(c["slots"].astype(np.int32)).cuda()
+    ref = pcr.KVPool(c["pk"].cuda(), c["pv"].cuda(), Hkv, d)
+    qr, kr = torch.empty_like(c["qd"]), torch.empty_like(c["kd"])
+    pcr.rope_rows(c["rope"], c["qd"], posd, qr)
+    pcr.rope_rows(c["rope"], c["kd"], posd, kr)
+    pcr.append_kv(ref, kr, c["vd"], slots)
+    pool = pcr.KVPool(c["pk"].cuda(), c["pv"].cuda(), Hkv, d)
+    qi = c["qd"].clone()
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    pcr.rope_append_kv(c["rope"], pool, qi, c["kd"], c["vd"], posd, slots, Hq, qi, stream=st)
+    st.synchronize()
+    assert torch.equal(qi, qr) and torch.equal(pool.k, ref.k) and torch.equal(pool.v, ref.v)
+    q_out = torch.zeros_like(qr)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        pcr.rope_append_kv(c["rope"], pool, c["qd"], c["kd"], c["vd"], posd, slots, Hq, q_out)
+    for _ in range(3):
+        q_out.zero_()
+        pool.k.copy_(c["pk"])
+        pool.v.copy_(c["pv"])
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(q_out, qr) and torch.equal(pool.k, ref.k) and torch.equal(pool.v, ref.v)
+
+
+def test_infinities_and_nan_stay_in_their_pairs():
+    T, H, d = 3, 2, 64
+    x = torch.ones(T, H, d, dtype=torch.bfloat16)
+    x[1, 0, 5], x[2, 1, 40] = float("nan"), float("inf")
+    f, axis = _rotation(64, 1)
+    out = torch.empty(T, H, d, dtype=torch.bfloat16, device="cuda")
+    pcr.rope_rows(pcr.Rope(f, axis), x.cuda(), torch.tensor([[3, 4, 5]], dtype=torch.int32).cuda(), out)
+    bad = ~torch.isfinite(out.cpu().float())
+    where = {tuple(i) for i in bad.nonzero().tolist()}
+    assert where == {(1, 0, 5), (1, 0, 37), (2, 1, 8), (2, 1, 40)}
