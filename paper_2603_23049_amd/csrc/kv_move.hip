@@ -7,6 +7,7 @@
 // rather than touching memory outside the pool.
 #include <type_traits>
 
+#include "append_tile.h"
 #include "pcr_internal.h"
 
 namespace pcr {
@@ -66,10 +67,7 @@ __global__ __launch_bounds__(256) void append_kv_kernel(
     const u16 *__restrict__ k_new, const u16 *__restrict__ v_new,
     const int32_t *__restrict__ slot_mapping, int32_t T)
 {
-    constexpr int EXT = kBlockSize - 1;        // tokens after the tile it may take
-    constexpr int ROWS = TILE + EXT;
-    static_assert(ROWS < 64, "one wave ranks the chunk runs");
-    static_assert(TILE >= kBlockSize, "a tile starts a block");
+    constexpr int EXT = append_tile::kExt, ROWS = TILE + EXT;
     constexpr int CPR = D / 8;                 // 16-B chunks per row
     constexpr int NCH = (TILE * CPR + 255) / 256;
     static_assert(EXT * CPR <= 256, "one chunk of the rows after the tile per thread");
@@ -113,24 +111,8 @@ __global__ __launch_bounds__(256) void append_kv_kernel(
     int32_t sl = -1;                           // wave 0: the slot of token tok0 + tid
     bool follows = false;                      // and whether it follows the token before's
     if (tid < 64) {
-        // Lane 63 reads the slot of the token before the tile (all slots in one load).
-        const int t = tid == 63 ? tok0 - 1 : tok0 + tid;
-        if ((tid < ROWS || tid == 63) && t >= 0 && t < T) {
-            sl = slot_mapping[t];
-            if (sl < 0 || sl / kBlockSize >= num_blocks) sl = -1;
-        }
-        // the slot of the token before this one (the wave rotated by one lane: DPP wave_ror:1)
-        const int32_t before = __builtin_amdgcn_update_dpp(sl, sl, 0x13C, 0xf, 0xf, false);
-        if (tid == 63) sl = -1;
-        follows = sl >= 0 && before >= 0 && sl == before + 1;
-        // heads: tokens that do not go on inside the block of the token before them. The
-        // tile's own tokens run from its first head to the first head at or after its end
-        // (both within 15 tokens: a block has 16 slots).
-        const uint64_t heads = ~__builtin_amdgcn_ballot_w64(follows && sl % kBlockSize != 0);
-        const uint64_t rest = heads >> TILE;
-        const int first = (int)__builtin_ctzll(heads);
-        const int last = rest ? min(ROWS, TILE + (int)__builtin_ctzll(rest)) : ROWS;
-        if (tid < first || tid >= last) sl = -1;
+        int last;
+        append_tile::own_slots<TILE>(slot_mapping, T, num_blocks, tok0, sl, follows, last);
         if (tid < ROWS) slots[tid] = sl;
         if (tid == 0) n_rows = last;
     }
@@ -147,23 +129,7 @@ __global__ __launch_bounds__(256) void append_kv_kernel(
     if constexpr (!EARLY) {
         if (ext) load_ext();
     }
-    if (tid < 64) {                            // wave 0: the chunk runs
-        // A token starts a chunk run when its slot is valid and either opens an aligned chunk
-        // of 8 slots or does not follow the previous token's slot; the run goes on over the
-        // following tokens until the next start or invalid slot (a continuing token's slot
-        // is its predecessor's plus one, inside the same chunk).
-        const bool valid = sl >= 0;
-        const bool start = valid && (tid == 0 || sl % 8 == 0 || !follows);
-        const uint64_t starts = __builtin_amdgcn_ballot_w64(start);
-        const uint64_t stops = starts | ~__builtin_amdgcn_ballot_w64(valid);   // bits past ROWS are stops
-        if (start) {
-            const uint64_t after = tid == 63 ? 0ull : stops >> (tid + 1);
-            const int len = after ? 1 + __builtin_ctzll(after) : 64 - tid;
-            const int idx = __builtin_popcountll(starts & ((1ull << tid) - 1ull));
-            runs[idx] = (tid << 8) | len;
-        }
-        if (tid == 0) n_runs = __builtin_popcountll(starts);
-    }
+    if (tid < 64) append_tile::chunk_runs(sl, follows, runs, n_runs);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
         const int c = tid + 256 * i;
@@ -172,28 +138,7 @@ __global__ __launch_bounds__(256) void append_kv_kernel(
     if (ext) put_row(re, ce, ke, ve);
     __syncthreads();
 
-    // V: task = (run, dim)
-    const int nr = n_runs;
-    for (int task = tid; task < nr * D; task += 256) {
-        const int k = task / D, x = task % D;
-        const int rv = runs[k], r0 = rv >> 8, len = rv & 0xff;
-        const int32_t s0 = slots[r0];
-        const int64_t blk = s0 / kBlockSize, o = s0 % kBlockSize;
-        u16 *dst = pool_v + ((blk * Hkv + g) * D + x) * kBlockSize + o;
-        if (len == 8) {   // a whole aligned chunk (a run of 8 starts at a multiple of 8)
-            u16 e[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = vs[r0 + j][x];
-            u32x4 w;
-            w.x = e[0] | ((unsigned)e[1] << 16);
-            w.y = e[2] | ((unsigned)e[3] << 16);
-            w.z = e[4] | ((unsigned)e[5] << 16);
-            w.w = e[6] | ((unsigned)e[7] << 16);
-            *reinterpret_cast<u32x4 *>(dst) = w;
-        } else {
-            for (int j = 0; j < len; ++j) dst[j] = vs[r0 + j][x];
-        }
-    }
+    append_tile::put_v<D>(vs, slots, runs, n_runs, pool_v, Hkv, g);
 }
 
 // ---------------------------------------------------------------------------

@@ -5,87 +5,259 @@
 // positions lose their phase in fp32 (position 10^6 keeps 2^-4 of a radian), so the turn is
 // formed and reduced in fp64, in whole revolutions: r = position * (inv_freq / 2 pi),
 // minus its nearest integer, and cos and sin of the rest are taken in fp32.
+//
+// Bound by moving the rows. A thread takes one unit of a token, 8 pairs = two 16-byte
+// chunks of each head, computes their cos and sin once and walks the heads with them in
+// registers. With few tokens the heads are dealt to more workgroups, each of which
+// computes the angles again.
 #include <math.h>
 
+#include <type_traits>
+
+#include "append_tile.h"
 #include "pcr_internal.h"
 
 namespace pcr {
 namespace {
 
 typedef unsigned short u16;
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 128;
 constexpr int kMaxAxes = 4;
+constexpr int32_t kMaxTokens = 1 << 27;   // keeps every grid inside 2^32 threads
+constexpr int kUnit = 8;          // pairs of a unit
+constexpr int kTile = 32;         // new tokens of a K/V workgroup (append_tile.h)
 
 // The rotation, in the launch's arguments.
 struct RopeArgs {
     double turns[kMaxPairs];      // revolutions per position step
     uint8_t axis[kMaxPairs];
     int32_t half;                 // pairs
+    int32_t axes;
     int32_t interleaved;
     float scale, sin_scale;       // of cos and of sin (negated: transposed)
 };
 
-__device__ __forceinline__ float to_f32(u16 v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
-__device__ __forceinline__ u16 to_bf16(float v) { return __builtin_bit_cast(u16, (__bf16)v); }
+// One unit of one token: where its two chunks lie in a head's row, and its cos and sin.
+struct Unit {
+    int32_t at[2];                // element offsets
+    bool turned;                  // false: dims past the rotation, copied
+    float c[kUnit], s[kUnit];
+};
 
-__device__ __forceinline__ void turn(const RopeArgs &ra, const int32_t *positions, int64_t pos_stride, int64_t t, int j,
-                                     float *c, float *s)
+__device__ __forceinline__ void make_unit(const RopeArgs &ra, const int32_t *__restrict__ positions,
+                                          int64_t pos_stride, int64_t t, int u, Unit &un)
 {
-    double r = (double)positions[ra.axis[j] * pos_stride + t] * ra.turns[j];
-    r -= rint(r);
-    sincospif(2.f * (float)r, s, c);
-    *c *= ra.scale;
-    *s *= ra.sin_scale;
+    const int n = ra.half / kUnit;                     // turned units of a head
+    un.turned = u < n;
+    if (un.turned && !ra.interleaved) {
+        un.at[0] = kUnit * u;
+        un.at[1] = ra.half + kUnit * u;
+    } else {                                           // 16 dims back to back
+        un.at[0] = 2 * kUnit * u;
+        un.at[1] = un.at[0] + kUnit;
+    }
+    if (!un.turned) return;
+    int32_t p[kMaxAxes];
+#pragma unroll
+    for (int a = 0; a < kMaxAxes; ++a) p[a] = a < ra.axes ? positions[a * pos_stride + t] : 0;
+    const uint64_t axis = *reinterpret_cast<const uint64_t *>(ra.axis + kUnit * u);
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) {
+        const int a = (int)(axis >> (8 * j)) & 3;
+        const int32_t pa = a & 2 ? (a & 1 ? p[3] : p[2]) : (a & 1 ? p[1] : p[0]);
+        double r = (double)pa * ra.turns[kUnit * u + j];
+        r -= rint(r);
+        float s, c;
+        sincospif(2.f * (float)r, &s, &c);
+        un.c[j] = c * ra.scale;
+        un.s[j] = s * ra.sin_scale;
+    }
 }
 
-// Element x of a head's row after the rotation.
-__device__ __forceinline__ u16 rotated(const u16 *row, int x, const RopeArgs &ra, const int32_t *positions,
-                                       int64_t pos_stride, int64_t t)
+__device__ __forceinline__ f32x8 widen(u32x4 v) { return __builtin_convertvector(__builtin_bit_cast(bf16x8, v), f32x8); }
+__device__ __forceinline__ u32x4 narrow(f32x8 v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8)); }
+
+// The unit's two chunks of one head, rotated (fp32 products, rounded once).
+template <bool IL>
+__device__ __forceinline__ void rotate(const Unit &un, u32x4 &a, u32x4 &b)
 {
-    if (x >= 2 * ra.half) return row[x];
-    const int j = ra.interleaved ? x >> 1 : x % ra.half;
-    const bool second = ra.interleaved ? x & 1 : x >= ra.half;
-    const int i1 = ra.interleaved ? 2 * j : j, i2 = ra.interleaved ? 2 * j + 1 : j + ra.half;
-    float c, s;
-    turn(ra, positions, pos_stride, t, j, &c, &s);
-    const float a = to_f32(row[i1]), b = to_f32(row[i2]);
-    return to_bf16(second ? b * c + a * s : a * c - b * s);
+    const f32x8 x = widen(a), y = widen(b);
+    f32x8 r, w;
+    if constexpr (IL) {                                // chunk a holds pairs 0..3, b pairs 4..7
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            r[2 * j] = x[2 * j] * un.c[j] - x[2 * j + 1] * un.s[j];
+            r[2 * j + 1] = x[2 * j + 1] * un.c[j] + x[2 * j] * un.s[j];
+            w[2 * j] = y[2 * j] * un.c[4 + j] - y[2 * j + 1] * un.s[4 + j];
+            w[2 * j + 1] = y[2 * j + 1] * un.c[4 + j] + y[2 * j] * un.s[4 + j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            r[j] = x[j] * un.c[j] - y[j] * un.s[j];
+            w[j] = y[j] * un.c[j] + x[j] * un.s[j];
+        }
+    }
+    a = un.turned ? narrow(r) : a;
+    b = un.turned ? narrow(w) : b;
 }
 
-// One workgroup per token; the whole token is read before any of it is written (in place).
+// Heads [h0, h1) of the tokens of one workgroup. Threads past the last whole token idle.
+// (A thread reads a unit before it writes it, and no other touches it: in place is safe.)
+template <bool IL>
+__device__ __forceinline__ void rotate_rows(const RopeArgs &ra, const u16 *x, int64_t x_stride,
+                                            const int32_t *__restrict__ positions, int64_t pos_stride, int32_t T,
+                                            int32_t D, int tile, int h0, int h1, u16 *out, int64_t out_stride)
+{
+    const int units = D / (2 * kUnit), per = kThreads / units;
+    const int tl = threadIdx.x / units, u = threadIdx.x - tl * units;
+    const int64_t t = (int64_t)tile * per + tl;
+    if (tl >= per || t >= T) return;
+    Unit un;
+    make_unit(ra, positions, pos_stride, t, u, un);
+    const u16 *src = x + t * x_stride;
+    u16 *dst = out + t * out_stride;
+    constexpr int W = 4;                               // heads in flight
+    for (int h = h0; h < h1; h += W) {
+        u32x4 a[W], b[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const int hh = min(h + i, h1 - 1);         // (past the end: the last one again, not written)
+            a[i] = *reinterpret_cast<const u32x4 *>(src + hh * D + un.at[0]);
+            b[i] = *reinterpret_cast<const u32x4 *>(src + hh * D + un.at[1]);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            rotate<IL>(un, a[i], b[i]);
+            if (h + i < h1) {
+                *reinterpret_cast<u32x4 *>(dst + (h + i) * D + un.at[0]) = a[i];
+                *reinterpret_cast<u32x4 *>(dst + (h + i) * D + un.at[1]) = b[i];
+            }
+        }
+    }
+}
+
+// Grid (token tiles, head groups of `heads`).
+template <bool IL>
 __global__ __launch_bounds__(kThreads) void rope_rows_kernel(const RopeArgs ra, const u16 *x, int64_t x_stride,
                                                              const int32_t *__restrict__ positions, int64_t pos_stride,
-                                                             int32_t H, int32_t D, u16 *out, int64_t out_stride)
+                                                             int32_t T, int32_t H, int32_t D, int32_t heads, u16 *out,
+                                                             int64_t out_stride)
 {
-    const int64_t t = blockIdx.x;
-    for (int h = 0; h < H; ++h) {
-        const u16 *row = x + t * x_stride + (int64_t)h * D;
-        u16 *orow = out + t * out_stride + (int64_t)h * D;
-        const int e = threadIdx.x;
-        const u16 v = e < D ? rotated(row, e, ra, positions, pos_stride, t) : (u16)0;
-        __syncthreads();
-        if (e < D) orow[e] = v;
+    const int h0 = blockIdx.y * heads;
+    rotate_rows<IL>(ra, x, x_stride, positions, pos_stride, T, D, blockIdx.x, h0, min(H, h0 + heads), out, out_stride);
+}
+
+// What the K/V and Q workgroups of one launch share out.
+struct AppendArgs {
+    u16 *pool_k, *pool_v;
+    const u16 *k_new, *v_new, *q;
+    u16 *q_out;
+    int64_t k_stride, v_stride, q_stride, pos_stride;
+    const int32_t *positions, *slot_mapping;
+    int32_t num_blocks, Hkv, Hq, T;
+    int32_t kv_heads, kv_groups, kv_wgs;      // kv heads of a workgroup, groups of them, K/V workgroups
+    int32_t q_heads, q_groups;                // the same of Q
+};
+
+// K and V of kv heads [g0, g1) of one tile of new tokens: K rotated in registers and written
+// by rows, V through LDS into its d-major chunks.
+template <int D, bool IL>
+__device__ __forceinline__ void append_heads(const RopeArgs &ra, const AppendArgs &aa, int tile, int g0, int g1)
+{
+    constexpr int ROWS = kTile + append_tile::kExt, CPR = D / 8, UNITS = D / (2 * kUnit);
+    constexpr int NK = (ROWS * UNITS + kThreads - 1) / kThreads, NV = (ROWS * CPR + kThreads - 1) / kThreads;
+    __shared__ __attribute__((aligned(16))) u16 vs[2][ROWS][D + 8];   // +8 elements: stagger rows across banks
+    __shared__ int32_t slots[ROWS];            // -1: no slot, or another tile's
+    __shared__ int32_t runs[ROWS];
+    __shared__ int32_t n_runs;
+    const int tid = threadIdx.x, tok0 = tile * kTile;
+    if (tid < 64) {
+        int32_t sl;
+        bool follows;
+        int last;
+        append_tile::own_slots<kTile>(aa.slot_mapping, aa.T, aa.num_blocks, tok0, sl, follows, last);
+        if (tid < ROWS) slots[tid] = sl;
+        append_tile::chunk_runs(sl, follows, runs, n_runs);
+    }
+    __syncthreads();
+    Unit un[NK];
+    int64_t k_src[NK], k_dst[NK], v_src[NV];   // element offsets of kv head 0; -1: none
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+        const int c = tid + kThreads * i, r = c / UNITS, u = c % UNITS;
+        const int32_t slot = r < ROWS ? slots[r] : -1;
+        k_dst[i] = -1;
+        if (slot < 0) continue;
+        make_unit(ra, aa.positions, aa.pos_stride, tok0 + r, u, un[i]);
+        k_src[i] = (int64_t)(tok0 + r) * aa.k_stride;
+        k_dst[i] = ((int64_t)(slot / kBlockSize) * aa.Hkv * kBlockSize + slot % kBlockSize) * D;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = tid + kThreads * i, r = c / CPR;
+        v_src[i] = r < ROWS && slots[r] >= 0 ? (int64_t)(tok0 + r) * aa.v_stride + c % CPR * 8 : -1;
+    }
+    u32x4 ka[NK], kb[NK], vv[NV];
+    auto load = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            if (k_dst[i] < 0) continue;
+            ka[i] = *reinterpret_cast<const u32x4 *>(aa.k_new + k_src[i] + g * D + un[i].at[0]);
+            kb[i] = *reinterpret_cast<const u32x4 *>(aa.k_new + k_src[i] + g * D + un[i].at[1]);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (v_src[i] >= 0) vv[i] = *reinterpret_cast<const u32x4 *>(aa.v_new + v_src[i] + g * D);
+    };
+    load(g0);
+    for (int g = g0; g < g1; ++g) {
+        u16(*buf)[D + 8] = vs[(g - g0) & 1];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = tid + kThreads * i;
+            if (v_src[i] >= 0) *reinterpret_cast<u32x4 *>(&buf[c / CPR][c % CPR * 8]) = vv[i];
+        }
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            if (k_dst[i] < 0) continue;
+            rotate<IL>(un[i], ka[i], kb[i]);
+            u16 *dst = aa.pool_k + k_dst[i] + (int64_t)g * kBlockSize * D;
+            *reinterpret_cast<u32x4 *>(dst + un[i].at[0]) = ka[i];
+            *reinterpret_cast<u32x4 *>(dst + un[i].at[1]) = kb[i];
+        }
+        if (g + 1 < g1) load(g + 1);
+        __syncthreads();                       // (and every wave is through with the other buffer)
+        append_tile::put_v<D>(buf, slots, runs, n_runs, aa.pool_v, aa.Hkv, g);
     }
 }
 
-__global__ __launch_bounds__(kThreads) void rope_append_kernel(
-    const RopeArgs ra, u16 *__restrict__ pool_k, u16 *__restrict__ pool_v, int32_t num_blocks, int32_t Hkv, int32_t D,
-    const u16 *__restrict__ k_new, int64_t k_stride, const u16 *__restrict__ v_new, int64_t v_stride,
-    const int32_t *__restrict__ positions, int64_t pos_stride, const int32_t *__restrict__ slot_mapping)
+// The first kv_wgs workgroups append (they take longest), the others rotate Q.
+template <int D, bool IL>
+__global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs ra, const AppendArgs aa)
 {
-    const int64_t t = blockIdx.x;
-    const int32_t slot = slot_mapping[t];
-    if (slot < 0 || slot / kBlockSize >= num_blocks) return;
-    const int64_t blk = slot / kBlockSize;
-    const int o = slot % kBlockSize;
-    for (int i = threadIdx.x; i < Hkv * D; i += kThreads) {
-        const int g = i / D, e = i % D;
-        pool_k[((blk * Hkv + g) * kBlockSize + o) * D + e] =
-            rotated(k_new + t * k_stride + (int64_t)g * D, e, ra, positions, pos_stride, t);
-        pool_v[((blk * Hkv + g) * D + e) * kBlockSize + o] = v_new[t * v_stride + i];
+    if ((int)blockIdx.x < aa.kv_wgs) {
+        const int tile = blockIdx.x / aa.kv_groups, g0 = (blockIdx.x - tile * aa.kv_groups) * aa.kv_heads;
+        append_heads<D, IL>(ra, aa, tile, g0, min(aa.Hkv, g0 + aa.kv_heads));
+    } else {
+        const int w = blockIdx.x - aa.kv_wgs, tile = w / aa.q_groups, h0 = (w - tile * aa.q_groups) * aa.q_heads;
+        rotate_rows<IL>(ra, aa.q, aa.q_stride, aa.positions, aa.pos_stride, aa.T, D, tile, h0,
+                        min(aa.Hq, h0 + aa.q_heads), aa.q_out, (int64_t)aa.Hq * D);
     }
+}
+
+// Heads per workgroup, of H, where `tiles` workgroups would take all heads: enough workgroups
+// for the device, whole groups of heads otherwise.
+constexpr int kWantWgs = 1024;
+int32_t heads_per_wg(int64_t tiles, int32_t H)
+{
+    const int64_t groups = (kWantWgs + tiles - 1) / tiles;
+    return (int32_t)(groups >= H ? 1 : (H + groups - 1) / groups);
 }
 
 // The checks of a rotation, and its launch arguments.
@@ -99,6 +271,7 @@ pcr_status rope_args(const pcr_rope *rope, int32_t head_dim, int32_t inverse, co
         return fail(PCR_ERR_INVALID_ARG, "%s: num_axes must be 1 to %d", who, kMaxAxes);
     if (!isfinite(rope->scale)) return fail(PCR_ERR_INVALID_ARG, "%s: scale is not finite", who);
     ra->half = rope->rotary_dim / 2;
+    ra->axes = rope->num_axes;
     ra->interleaved = rope->interleaved != 0;
     ra->scale = rope->scale;
     ra->sin_scale = inverse ? -rope->scale : rope->scale;
@@ -118,6 +291,7 @@ pcr_status check_rows(const void *x, int64_t stride, int64_t width, const char *
 {
     if (!x) return fail(PCR_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
     if ((uintptr_t)x & 15) return fail(PCR_ERR_INVALID_ARG, "%s: %s must be 16-byte aligned", who, what);
+    if (width > (int64_t)1 << 30) return fail(PCR_ERR_UNSUPPORTED, "%s: rows of more than 2^30 elements", who);
     if (stride < width || stride % 8 || stride > (int64_t)1 << 40)
         return fail(PCR_ERR_INVALID_ARG, "%s: %s stride %lld is not a multiple of 8 of at least %lld", who, what,
                     (long long)stride, (long long)width);
@@ -135,8 +309,36 @@ hipError_t launch_rows(const RopeArgs &ra, const void *x, int64_t x_stride, cons
                        int64_t pos_stride, int32_t T, int32_t H, int32_t D, void *out, int64_t out_stride,
                        hipStream_t s)
 {
-    hipLaunchKernelGGL(rope_rows_kernel, dim3(T), dim3(kThreads), 0, s, ra, static_cast<const u16 *>(x), x_stride,
-                       positions, pos_stride, H, D, static_cast<u16 *>(out), out_stride);
+    const int per = kThreads / (D / (2 * kUnit));
+    const int64_t tiles = ((int64_t)T + per - 1) / per;
+    const int32_t heads = heads_per_wg(tiles, H);
+    const dim3 grid((unsigned)tiles, (unsigned)((H + heads - 1) / heads));
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, ra, static_cast<const u16 *>(x), x_stride, positions,
+                           pos_stride, T, H, D, heads, static_cast<u16 *>(out), out_stride);
+    };
+    if (ra.interleaved) launch(rope_rows_kernel<true>);
+    else launch(rope_rows_kernel<false>);
+    return hipGetLastError();
+}
+
+hipError_t launch_append(const RopeArgs &ra, AppendArgs aa, int D, hipStream_t s)
+{
+    const int per = kThreads / (D / (2 * kUnit));
+    const int64_t kv_tiles = ((int64_t)aa.T + kTile - 1) / kTile, q_tiles = ((int64_t)aa.T + per - 1) / per;
+    aa.kv_heads = heads_per_wg(kv_tiles, aa.Hkv);
+    aa.kv_groups = (aa.Hkv + aa.kv_heads - 1) / aa.kv_heads;
+    aa.kv_wgs = (int32_t)(kv_tiles * aa.kv_groups);
+    aa.q_heads = aa.Hq ? heads_per_wg(q_tiles, aa.Hq) : 1;
+    aa.q_groups = (aa.Hq + aa.q_heads - 1) / aa.q_heads;
+    const dim3 grid((unsigned)(aa.kv_wgs + q_tiles * aa.q_groups));
+    auto launch = [&](auto dim) {
+        constexpr int DD = decltype(dim)::value;
+        if (ra.interleaved) hipLaunchKernelGGL((rope_append_kernel<DD, true>), grid, dim3(kThreads), 0, s, ra, aa);
+        else hipLaunchKernelGGL((rope_append_kernel<DD, false>), grid, dim3(kThreads), 0, s, ra, aa);
+    };
+    if (D == 128) launch(std::integral_constant<int, 128>{});
+    else launch(std::integral_constant<int, 64>{});
     return hipGetLastError();
 }
 
@@ -160,6 +362,7 @@ pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, con
     st = rope_args(rope, pool->head_dim, 0, who, &ra);
     if (st) return st;
     if (T < 0 || num_q_heads < 0) return fail(PCR_ERR_INVALID_ARG, "%s: negative T or num_q_heads", who);
+    if (T > kMaxTokens) return fail(PCR_ERR_UNSUPPORTED, "%s: more than 2^27 tokens", who);
     if (num_q_heads % pool->num_kv_heads != 0)
         return fail(PCR_ERR_UNSUPPORTED, "%s: num_q_heads %d is not a multiple of num_kv_heads %d", who, num_q_heads,
                     pool->num_kv_heads);
@@ -178,17 +381,24 @@ pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, con
         if (!(q == q_out && q_stride == q_width) && rows_overlap(q, q_stride, q_out, q_width, T, q_width))
             return fail(PCR_ERR_INVALID_ARG, "%s: q and q_out overlap (and are not one array)", who);
     }
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = hipSuccess;
-    if (num_q_heads > 0)
-        e = launch_rows(ra, q, q_stride, positions, pos_stride, T, num_q_heads, pool->head_dim, q_out, q_width, s);
-    if (e == hipSuccess) {
-        hipLaunchKernelGGL(rope_append_kernel, dim3(T), dim3(kThreads), 0, s, ra, static_cast<u16 *>(pool->k),
-                           static_cast<u16 *>(pool->v), pool->num_blocks, pool->num_kv_heads, pool->head_dim,
-                           static_cast<const u16 *>(k_new), k_stride, static_cast<const u16 *>(v_new), v_stride,
-                           positions, pos_stride, slot_mapping);
-        e = hipGetLastError();
-    }
+    AppendArgs aa{};
+    aa.pool_k = static_cast<u16 *>(pool->k);
+    aa.pool_v = static_cast<u16 *>(pool->v);
+    aa.k_new = static_cast<const u16 *>(k_new);
+    aa.v_new = static_cast<const u16 *>(v_new);
+    aa.q = static_cast<const u16 *>(q);
+    aa.q_out = static_cast<u16 *>(q_out);
+    aa.k_stride = k_stride;
+    aa.v_stride = v_stride;
+    aa.q_stride = q_stride;
+    aa.pos_stride = pos_stride;
+    aa.positions = positions;
+    aa.slot_mapping = slot_mapping;
+    aa.num_blocks = pool->num_blocks;
+    aa.Hkv = pool->num_kv_heads;
+    aa.Hq = num_q_heads;
+    aa.T = T;
+    const hipError_t e = launch_append(ra, aa, pool->head_dim, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "pcr_rope_append_kv: launch");
     return PCR_OK;
 }
@@ -206,6 +416,7 @@ pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, 
     RopeArgs ra;
     pcr_status st = rope_args(rope, head_dim, inverse, who, &ra);
     if (st || T == 0) return st;
+    if (T > kMaxTokens) return fail(PCR_ERR_UNSUPPORTED, "%s: more than 2^27 tokens", who);
     if (!positions) return fail(PCR_ERR_INVALID_ARG, "%s: positions is NULL", who);
     if (pos_stride < T && rope->num_axes > 1)
         return fail(PCR_ERR_INVALID_ARG, "%s: pos_stride %lld < T", who, (long long)pos_stride);

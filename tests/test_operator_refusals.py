@@ -93,7 +93,7 @@ def test_append_rows():
         if kw == dict(out=A):
             kw = dict(out=A, qs=264)                 # the same array, but not back to back
         assert _append(**kw) == INV, kw
-    assert _append(Hq=3) == UNS
+    assert _append(Hq=3) == UNS and _append(T=2 ** 27 + 1, ps=2 ** 28) == UNS
     assert _append(pool=_pool(d=96)) == UNS and _append(pool=_pool(bs=8)) == UNS
     assert pcr.lib().pcr_rope_append_kv(None, _pool(), A, 256, A, 128, A, 128, A, 10, A, 10, 4, A << 8, None) == INV
 
@@ -102,6 +102,7 @@ def test_plain_rows():
     for kw in (dict(H=0), dict(x=None), dict(out=None), dict(xs=120), dict(os=127), dict(x=A + 2), dict(out=A + 256),
                dict(out=A, os=136)):
         assert _rows(**kw) == INV, kw
+    assert _rows(T=2 ** 27 + 1, ps=2 ** 28) == UNS and _rows(H=2 ** 25, xs=2 ** 31, os=2 ** 31) == UNS
     for d in (0, 8, 72, 272, -16):
         assert _rows(d=d) == UNS
     assert _rows(rope=_rope(rd=64), d=48) == UNS
