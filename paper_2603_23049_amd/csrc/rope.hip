@@ -4,7 +4,9 @@
 // Pair j of a token's head turns by positions[axis_j] * inv_freq[j]. Angles of far
 // positions lose their phase in fp32 (position 10^6 keeps 2^-4 of a radian), so the turn is
 // formed and reduced in fp64, in whole revolutions: r = position * (inv_freq / 2 pi),
-// minus its nearest integer, and cos and sin of the rest are taken in fp32.
+// minus its nearest integer, and cos and sin of the rest come from v_cos_f32 and v_sin_f32,
+// which take revolutions (off by at most 2^-22.9 on 2^28 arguments of [-1/2, 1/2], against
+// fp64; the library's sincospif, 2^-24.2, takes about twice the instructions).
 //
 // Bound by moving the rows. A thread takes one unit of a token, 8 pairs = two 16-byte
 // chunks of each head, computes their cos and sin once and walks the heads with them in
@@ -12,6 +14,7 @@
 // computes the angles again.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "append_tile.h"
@@ -42,6 +45,21 @@ struct RopeArgs {
     float scale, sin_scale;       // of cos and of sin (negated: transposed)
 };
 
+// NT: past the caches.
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(const u16 *p)
+{
+    auto *v = reinterpret_cast<const u32x4 *>(p);
+    if constexpr (NT) return __builtin_nontemporal_load(v);
+    return *v;
+}
+template <bool NT>
+__device__ __forceinline__ void store16(u16 *p, u32x4 x)
+{
+    if constexpr (NT) __builtin_nontemporal_store(x, reinterpret_cast<u32x4 *>(p));
+    else *reinterpret_cast<u32x4 *>(p) = x;
+}
+
 // One unit of one token: where its two chunks lie in a head's row, and its cos and sin.
 struct Unit {
     int32_t at[2];                // element offsets
@@ -49,8 +67,7 @@ struct Unit {
     float c[kUnit], s[kUnit];
 };
 
-__device__ __forceinline__ void make_unit(const RopeArgs &ra, const int32_t *__restrict__ positions,
-                                          int64_t pos_stride, int64_t t, int u, Unit &un)
+__device__ __forceinline__ void place_unit(const RopeArgs &ra, int u, Unit &un)
 {
     const int n = ra.half / kUnit;                     // turned units of a head
     un.turned = u < n;
@@ -61,6 +78,11 @@ __device__ __forceinline__ void make_unit(const RopeArgs &ra, const int32_t *__r
         un.at[0] = 2 * kUnit * u;
         un.at[1] = un.at[0] + kUnit;
     }
+}
+
+__device__ __forceinline__ void turn_unit(const RopeArgs &ra, const int32_t *__restrict__ positions,
+                                          int64_t pos_stride, int64_t t, int u, Unit &un)
+{
     if (!un.turned) return;
     int32_t p[kMaxAxes];
 #pragma unroll
@@ -72,10 +94,8 @@ __device__ __forceinline__ void make_unit(const RopeArgs &ra, const int32_t *__r
         const int32_t pa = a & 2 ? (a & 1 ? p[3] : p[2]) : (a & 1 ? p[1] : p[0]);
         double r = (double)pa * ra.turns[kUnit * u + j];
         r -= rint(r);
-        float s, c;
-        sincospif(2.f * (float)r, &s, &c);
-        un.c[j] = c * ra.scale;
-        un.s[j] = s * ra.sin_scale;
+        un.c[j] = __builtin_amdgcn_cosf((float)r) * ra.scale;
+        un.s[j] = __builtin_amdgcn_sinf((float)r) * ra.sin_scale;
     }
 }
 
@@ -109,48 +129,55 @@ __device__ __forceinline__ void rotate(const Unit &un, u32x4 &a, u32x4 &b)
 
 // Heads [h0, h1) of the tokens of one workgroup. Threads past the last whole token idle.
 // (A thread reads a unit before it writes it, and no other touches it: in place is safe.)
-template <bool IL>
+template <bool IL, int THREADS, int W, bool NT>
 __device__ __forceinline__ void rotate_rows(const RopeArgs &ra, const u16 *x, int64_t x_stride,
                                             const int32_t *__restrict__ positions, int64_t pos_stride, int32_t T,
                                             int32_t D, int tile, int h0, int h1, u16 *out, int64_t out_stride)
 {
-    const int units = D / (2 * kUnit), per = kThreads / units;
+    const int units = D / (2 * kUnit), per = THREADS / units;
     const int tl = threadIdx.x / units, u = threadIdx.x - tl * units;
     const int64_t t = (int64_t)tile * per + tl;
     if (tl >= per || t >= T) return;
     Unit un;
-    make_unit(ra, positions, pos_stride, t, u, un);
+    place_unit(ra, u, un);
     const u16 *src = x + t * x_stride;
     u16 *dst = out + t * out_stride;
-    constexpr int W = 4;                               // heads in flight
-    for (int h = h0; h < h1; h += W) {
-        u32x4 a[W], b[W];
+    u32x4 a[W], b[W];                                  // W heads in flight
+    auto load = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             const int hh = min(h + i, h1 - 1);         // (past the end: the last one again, not written)
-            a[i] = *reinterpret_cast<const u32x4 *>(src + hh * D + un.at[0]);
-            b[i] = *reinterpret_cast<const u32x4 *>(src + hh * D + un.at[1]);
+            a[i] = load16<NT>(src + (int64_t)hh * D + un.at[0]);
+            b[i] = load16<NT>(src + (int64_t)hh * D + un.at[1]);
         }
+    };
+    load(h0);                                          // in flight while the angles are formed
+    turn_unit(ra, positions, pos_stride, t, u, un);
+    for (int h = h0;;) {
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             rotate<IL>(un, a[i], b[i]);
             if (h + i < h1) {
-                *reinterpret_cast<u32x4 *>(dst + (h + i) * D + un.at[0]) = a[i];
-                *reinterpret_cast<u32x4 *>(dst + (h + i) * D + un.at[1]) = b[i];
+                store16<NT>(dst + (int64_t)(h + i) * D + un.at[0], a[i]);
+                store16<NT>(dst + (int64_t)(h + i) * D + un.at[1], b[i]);
             }
         }
+        h += W;
+        if (h >= h1) break;
+        load(h);
     }
 }
 
 // Grid (token tiles, head groups of `heads`).
-template <bool IL>
+template <bool IL, int W, bool NT>
 __global__ __launch_bounds__(kThreads) void rope_rows_kernel(const RopeArgs ra, const u16 *x, int64_t x_stride,
                                                              const int32_t *__restrict__ positions, int64_t pos_stride,
                                                              int32_t T, int32_t H, int32_t D, int32_t heads, u16 *out,
                                                              int64_t out_stride)
 {
     const int h0 = blockIdx.y * heads;
-    rotate_rows<IL>(ra, x, x_stride, positions, pos_stride, T, D, blockIdx.x, h0, min(H, h0 + heads), out, out_stride);
+    rotate_rows<IL, kThreads, W, NT>(ra, x, x_stride, positions, pos_stride, T, D, blockIdx.x, h0, min(H, h0 + heads), out,
+                                 out_stride);
 }
 
 // What the K/V and Q workgroups of one launch share out.
@@ -166,8 +193,9 @@ struct AppendArgs {
 };
 
 // K and V of kv heads [g0, g1) of one tile of new tokens: K rotated in registers and written
-// by rows, V through LDS into its d-major chunks.
-template <int D, bool IL>
+// by rows, V through LDS into its d-major chunks (two buffers, so a head costs one barrier). The
+// next head's rows are requested before this one's V leaves LDS.
+template <int D, bool IL, bool NT>
 __device__ __forceinline__ void append_heads(const RopeArgs &ra, const AppendArgs &aa, int tile, int g0, int g1)
 {
     constexpr int ROWS = kTile + append_tile::kExt, CPR = D / 8, UNITS = D / (2 * kUnit);
@@ -177,6 +205,26 @@ __device__ __forceinline__ void append_heads(const RopeArgs &ra, const AppendArg
     __shared__ int32_t runs[ROWS];
     __shared__ int32_t n_runs;
     const int tid = threadIdx.x, tok0 = tile * kTile;
+    Unit un[NK];
+    bool k_on[NK], v_on[NV];                   // rows this thread loads of
+    u32x4 ka[NK], kb[NK], vv[NV];
+    auto load = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            if (!k_on[i]) continue;
+            const u16 *src = aa.k_new + (int64_t)(tok0 + (tid + kThreads * i) / UNITS) * aa.k_stride + g * D;
+            ka[i] = load16<NT>(src + un[i].at[0]);
+            kb[i] = load16<NT>(src + un[i].at[1]);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = tid + kThreads * i;
+            if (v_on[i])
+                vv[i] = load16<NT>(aa.v_new + (int64_t)(tok0 + c / CPR) * aa.v_stride + g * D + c % CPR * 8);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < NK; ++i) place_unit(ra, (tid + kThreads * i) % UNITS, un[i]);
     if (tid < 64) {
         int32_t sl;
         bool follows;
@@ -186,46 +234,35 @@ __device__ __forceinline__ void append_heads(const RopeArgs &ra, const AppendArg
         append_tile::chunk_runs(sl, follows, runs, n_runs);
     }
     __syncthreads();
-    Unit un[NK];
-    int64_t k_src[NK], k_dst[NK], v_src[NV];   // element offsets of kv head 0; -1: none
+    int64_t k_dst[NK];
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
-        const int c = tid + kThreads * i, r = c / UNITS, u = c % UNITS;
+        const int r = (tid + kThreads * i) / UNITS;
         const int32_t slot = r < ROWS ? slots[r] : -1;
-        k_dst[i] = -1;
-        if (slot < 0) continue;
-        make_unit(ra, aa.positions, aa.pos_stride, tok0 + r, u, un[i]);
-        k_src[i] = (int64_t)(tok0 + r) * aa.k_stride;
+        k_on[i] = slot >= 0;
         k_dst[i] = ((int64_t)(slot / kBlockSize) * aa.Hkv * kBlockSize + slot % kBlockSize) * D;
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = tid + kThreads * i, r = c / CPR;
-        v_src[i] = r < ROWS && slots[r] >= 0 ? (int64_t)(tok0 + r) * aa.v_stride + c % CPR * 8 : -1;
+        const int r = (tid + kThreads * i) / CPR;
+        v_on[i] = r < ROWS && slots[r] >= 0;
     }
-    u32x4 ka[NK], kb[NK], vv[NV];
-    auto load = [&](int g) __attribute__((always_inline)) {
+    load(g0);                                  // in flight while the angles are formed
 #pragma unroll
-        for (int i = 0; i < NK; ++i) {
-            if (k_dst[i] < 0) continue;
-            ka[i] = *reinterpret_cast<const u32x4 *>(aa.k_new + k_src[i] + g * D + un[i].at[0]);
-            kb[i] = *reinterpret_cast<const u32x4 *>(aa.k_new + k_src[i] + g * D + un[i].at[1]);
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (v_src[i] >= 0) vv[i] = *reinterpret_cast<const u32x4 *>(aa.v_new + v_src[i] + g * D);
-    };
-    load(g0);
+    for (int i = 0; i < NK; ++i) {
+        const int c = tid + kThreads * i;
+        if (k_on[i]) turn_unit(ra, aa.positions, aa.pos_stride, tok0 + c / UNITS, c % UNITS, un[i]);
+    }
     for (int g = g0; g < g1; ++g) {
         u16(*buf)[D + 8] = vs[(g - g0) & 1];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = tid + kThreads * i;
-            if (v_src[i] >= 0) *reinterpret_cast<u32x4 *>(&buf[c / CPR][c % CPR * 8]) = vv[i];
+            if (v_on[i]) *reinterpret_cast<u32x4 *>(&buf[c / CPR][c % CPR * 8]) = vv[i];
         }
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-            if (k_dst[i] < 0) continue;
+            if (!k_on[i]) continue;
             rotate<IL>(un[i], ka[i], kb[i]);
             u16 *dst = aa.pool_k + k_dst[i] + (int64_t)g * kBlockSize * D;
             *reinterpret_cast<u32x4 *>(dst + un[i].at[0]) = ka[i];
@@ -238,27 +275,82 @@ __device__ __forceinline__ void append_heads(const RopeArgs &ra, const AppendArg
 }
 
 // The first kv_wgs workgroups append (they take longest), the others rotate Q.
-template <int D, bool IL>
+template <int D, bool IL, bool NT>
 __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs ra, const AppendArgs aa)
 {
     if ((int)blockIdx.x < aa.kv_wgs) {
         const int tile = blockIdx.x / aa.kv_groups, g0 = (blockIdx.x - tile * aa.kv_groups) * aa.kv_heads;
-        append_heads<D, IL>(ra, aa, tile, g0, min(aa.Hkv, g0 + aa.kv_heads));
+        append_heads<D, IL, NT>(ra, aa, tile, g0, min(aa.Hkv, g0 + aa.kv_heads));
     } else {
         const int w = blockIdx.x - aa.kv_wgs, tile = w / aa.q_groups, h0 = (w - tile * aa.q_groups) * aa.q_heads;
-        rotate_rows<IL>(ra, aa.q, aa.q_stride, aa.positions, aa.pos_stride, aa.T, D, tile, h0,
-                        min(aa.Hq, h0 + aa.q_heads), aa.q_out, (int64_t)aa.Hq * D);
+        rotate_rows<IL, kThreads, 4, NT>(ra, aa.q, aa.q_stride, aa.positions, aa.pos_stride, aa.T, D, tile, h0,
+                                         min(aa.Hq, h0 + aa.q_heads), aa.q_out, (int64_t)aa.Hq * D);
     }
 }
 
-// Heads per workgroup, of H, where `tiles` workgroups would take all heads: enough workgroups
-// for the device, whole groups of heads otherwise.
-constexpr int kWantWgs = 1024;
-int32_t heads_per_wg(int64_t tiles, int32_t H)
+// The same for few tokens, which wait on latency: single waves, one unit of one (token, head) a
+// thread, V in 2-byte stores straight from the registers. No barrier, and the stores of many
+// one-token sequences, each 2 bytes of a line of its own, come from many compute units.
+constexpr int kRowThreads = 64;
+template <int D, bool IL>
+__global__ __launch_bounds__(kRowThreads) void rope_append_rows_kernel(const RopeArgs ra, const AppendArgs aa)
 {
-    const int64_t groups = (kWantWgs + tiles - 1) / tiles;
-    return (int32_t)(groups >= H ? 1 : (H + groups - 1) / groups);
+    constexpr int UNITS = D / (2 * kUnit), PER = kRowThreads / UNITS;
+    if ((int)blockIdx.x < aa.kv_wgs) {
+        const int64_t pair = (int64_t)blockIdx.x * PER + threadIdx.x / UNITS;   // heads of a token side by side
+        const int u = threadIdx.x % UNITS, t = (int)(pair / aa.Hkv), g = (int)(pair - (int64_t)t * aa.Hkv);
+        if (t >= aa.T) return;
+        Unit un;
+        place_unit(ra, u, un);
+        const int32_t slot = aa.slot_mapping[t];
+        const u16 *ks = aa.k_new + t * aa.k_stride + g * D, *vs = aa.v_new + t * aa.v_stride + g * D + 16 * u;
+        u32x4 a = *reinterpret_cast<const u32x4 *>(ks + un.at[0]), b = *reinterpret_cast<const u32x4 *>(ks + un.at[1]);
+        u32x4 v[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vs + 8 * i);
+        turn_unit(ra, aa.positions, aa.pos_stride, t, u, un);
+        if (slot < 0 || slot / kBlockSize >= aa.num_blocks) return;
+        const int64_t payload = ((int64_t)(slot / kBlockSize) * aa.Hkv + g) * kBlockSize * D;
+        const int o = slot % kBlockSize;
+        rotate<IL>(un, a, b);
+        *reinterpret_cast<u32x4 *>(aa.pool_k + payload + o * D + un.at[0]) = a;
+        *reinterpret_cast<u32x4 *>(aa.pool_k + payload + o * D + un.at[1]) = b;
+        u16 *dst = aa.pool_v + payload + 16 * u * kBlockSize + o;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                dst[(8 * i + j) * kBlockSize] = (u16)(v[i][j >> 1] >> (16 * (j & 1)));
+    } else {
+        const int w = blockIdx.x - aa.kv_wgs, tile = w / aa.Hq, h = w - tile * aa.Hq;
+        rotate_rows<IL, kRowThreads, 1, false>(ra, aa.q, aa.q_stride, aa.positions, aa.pos_stride, aa.T, D, tile, h, h + 1,
+                                        aa.q_out, (int64_t)aa.Hq * D);
+    }
 }
+
+// Heads of a workgroup that walks several (rotate_rows): one batch of loads. Bytes in flight
+// come from many workgroups rather than from long ones: 18480 tokens of 32 query heads of 128
+// took 78 us with 4 heads, 82 with 8, 94 with 16 (16000 of 64 heads 109, 113, 127). Where that
+// gives fewer than kMinWgs workgroups every head has one of its own (300 rows of 64 heads of
+// 128: 3.8 us, 4.2 with twice the line).
+constexpr int kHeads = 4;
+constexpr int kMinWgs = 256;
+// K/V workgroups wanted; a tile's kv heads are dealt to as many as that takes (2048 to 8192 alike).
+constexpr int kKvWgs = 2048;
+// Bytes of K and Q up to which a call runs as rows (rope_append_rows_kernel). One token of each
+// of 64 sequences, 32 query / 8 kv heads of 128: 3.4 us as rows, 8.3 in tiles; 64 of one
+// sequence 3.4 and 4.9; 200 4.8 and 9.5, 4.4 and 5.1; 400 (the line) 7.2 and 11.2, 6.2 and 5.8;
+// 800 12.0 and 13.4, 10.9 and 7.3. With 8 / 1 heads 1600 tokens 5.3 and 10.0, 3.5 and 5.5.
+constexpr int64_t kRowsBytes = 4ll << 20;
+// Bytes of input above which it is read, and Q written, past the caches: input and output no
+// longer fit the 256 MB cache together. 18480 tokens as above (227 MB in) 92 -> 78 us =
+// 5.8 TB/s, with input in or out of the caches; 16384 rows of 40 heads of 128 (168 MB) 69 -> 64
+// out of them, 65 -> 63 in them. Below, 8000 tokens (98 MB) just written by the pass before
+// would take 38 instead of 34 (out of the caches 38 instead of 42). Only where each chunk's
+// wave stores whole lines (runs of 64 pairs, or more of them back to back): 8065 rows of 80 dims
+// would take 15 instead of 12 us.
+constexpr int64_t kNtBytes = 128ll << 20;
+bool whole_lines(const RopeArgs &ra) { return !ra.interleaved && ra.half % 64 == 0; }
 
 // The checks of a rotation, and its launch arguments.
 pcr_status rope_args(const pcr_rope *rope, int32_t head_dim, int32_t inverse, const char *who, RopeArgs *ra)
@@ -311,31 +403,54 @@ hipError_t launch_rows(const RopeArgs &ra, const void *x, int64_t x_stride, cons
 {
     const int per = kThreads / (D / (2 * kUnit));
     const int64_t tiles = ((int64_t)T + per - 1) / per;
-    const int32_t heads = heads_per_wg(tiles, H);
+    const int32_t heads = H >= kHeads && tiles * ((H + kHeads - 1) / kHeads) >= kMinWgs ? kHeads : 1;
     const dim3 grid((unsigned)tiles, (unsigned)((H + heads - 1) / heads));
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, ra, static_cast<const u16 *>(x), x_stride, positions,
                            pos_stride, T, H, D, heads, static_cast<u16 *>(out), out_stride);
     };
-    if (ra.interleaved) launch(rope_rows_kernel<true>);
-    else launch(rope_rows_kernel<false>);
+    if (whole_lines(ra) && (int64_t)T * H * D * 2 > kNtBytes) launch(rope_rows_kernel<false, 4, true>);
+    else if (heads > 1 && ra.interleaved) launch(rope_rows_kernel<true, 4, false>);
+    else if (heads > 1) launch(rope_rows_kernel<false, 4, false>);
+    else if (ra.interleaved) launch(rope_rows_kernel<true, 1, false>);
+    else launch(rope_rows_kernel<false, 1, false>);
     return hipGetLastError();
 }
 
 hipError_t launch_append(const RopeArgs &ra, AppendArgs aa, int D, hipStream_t s)
 {
+    if ((int64_t)aa.T * (aa.Hkv + aa.Hq) * D * 2 <= kRowsBytes) {
+        const int rows = kRowThreads / (D / (2 * kUnit));
+        aa.kv_wgs = (int32_t)(((int64_t)aa.T * aa.Hkv + rows - 1) / rows);
+        const dim3 grid((unsigned)(aa.kv_wgs + (aa.T + rows - 1) / rows * aa.Hq));
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, s, ra, aa); };
+        if (D == 128) {
+            if (ra.interleaved) go(rope_append_rows_kernel<128, true>);
+            else go(rope_append_rows_kernel<128, false>);
+        } else {
+            if (ra.interleaved) go(rope_append_rows_kernel<64, true>);
+            else go(rope_append_rows_kernel<64, false>);
+        }
+        return hipGetLastError();
+    }
     const int per = kThreads / (D / (2 * kUnit));
     const int64_t kv_tiles = ((int64_t)aa.T + kTile - 1) / kTile, q_tiles = ((int64_t)aa.T + per - 1) / per;
-    aa.kv_heads = heads_per_wg(kv_tiles, aa.Hkv);
+    const int64_t kv_groups = (kKvWgs + kv_tiles - 1) / kv_tiles;
+    aa.kv_heads = (int32_t)((aa.Hkv + kv_groups - 1) / kv_groups);
     aa.kv_groups = (aa.Hkv + aa.kv_heads - 1) / aa.kv_heads;
     aa.kv_wgs = (int32_t)(kv_tiles * aa.kv_groups);
-    aa.q_heads = aa.Hq ? heads_per_wg(q_tiles, aa.Hq) : 1;
+    aa.q_heads = kHeads;
     aa.q_groups = (aa.Hq + aa.q_heads - 1) / aa.q_heads;
+    const int64_t in_bytes = (int64_t)aa.T * (aa.Hq + 2 * aa.Hkv) * D * 2;
     const dim3 grid((unsigned)(aa.kv_wgs + q_tiles * aa.q_groups));
     auto launch = [&](auto dim) {
         constexpr int DD = decltype(dim)::value;
-        if (ra.interleaved) hipLaunchKernelGGL((rope_append_kernel<DD, true>), grid, dim3(kThreads), 0, s, ra, aa);
-        else hipLaunchKernelGGL((rope_append_kernel<DD, false>), grid, dim3(kThreads), 0, s, ra, aa);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, ra, aa); };
+        if constexpr (DD == 128) {            // (64 dims have no 64 pairs)
+            if (whole_lines(ra) && in_bytes > kNtBytes) return go(rope_append_kernel<DD, false, true>);
+        }
+        if (ra.interleaved) go(rope_append_kernel<DD, true, false>);
+        else go(rope_append_kernel<DD, false, false>);
     };
     if (D == 128) launch(std::integral_constant<int, 128>{});
     else launch(std::integral_constant<int, 64>{});
