@@ -7,6 +7,12 @@
 // slot. The token at a block's first slot writes the block's table entry: a new block's
 // first token is always one of the new tokens.
 //
+// Every workgroup forms the sums of all sequences itself (they are few, and their lengths stay
+// in the caches) and takes one tile of the rows: no workgroup waits for another, nothing is
+// kept between launches. The step's state (sums, lengths, counts) is written by the first
+// workgroup, unless it is updated in place while others still read it: then by a launch of
+// one workgroup after them.
+//
 // Sums saturate at 2^31 - 1 (a saturating sum of non-negative numbers does not depend on
 // the grouping), so no length, however wrong, wraps around into a fit.
 #include "pcr_internal.h"
@@ -14,182 +20,225 @@
 namespace pcr {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
 constexpr uint32_t kSumMax = 0x7FFFFFFFu;
 constexpr int32_t kMaxCount = 1 << 30;      // sequences, free ids, rows: below the saturated sum
 
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, kSumMax); }
 
-// Blocks that hold n tokens (n >= 0, up to 2^31 - 1 and beyond it for a sum of two).
+// Blocks that hold n tokens.
 __device__ __forceinline__ int64_t blocks_of(int64_t n) { return (n + kBlockSize - 1) / kBlockSize; }
 
-// Inclusive saturating sums of v over the workgroup's threads; *total gets the sum of all.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *wave_sum, uint32_t *total)
+// Inclusive saturating sums of N values over the workgroup's threads. One barrier; wave_sum
+// must not be written again before the next one.
+template <int THREADS, int N>
+__device__ __forceinline__ void block_scan(uint32_t (&v)[N], uint32_t (*wave_sum)[THREADS / 64])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t u = __shfl_up(v, off);
-        if (lane >= off) v = sat_add(v, u);
+        uint32_t u[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = __shfl_up(v[i], off);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = lane >= off ? sat_add(v[i], u[i]) : v[i];
     }
-    if (lane == 63) wave_sum[wave] = v;
-    __syncthreads();
-    uint32_t before = 0, all = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        const uint32_t u = wave_sum[w];
-        before = w < wave ? sat_add(before, u) : before;
-        all = sat_add(all, u);
+    if (lane == 63) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) wave_sum[i][wave] = v[i];
     }
     __syncthreads();
-    *total = all;
-    return sat_add(before, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint32_t before = 0;
+        for (int w = 0; w < THREADS / 64; ++w) before = w < wave ? sat_add(before, wave_sum[i][w]) : before;
+        v[i] = sat_add(before, v[i]);
+    }
 }
 
-// One workgroup: sequences in chunks of its threads, each chunk's sums first, then its tokens.
-__global__ __launch_bounds__(kThreads) void assign_kernel(
-    int32_t B, const int32_t *prefix_lens, const int32_t *__restrict__ suffix_lens,
-    int32_t *block_tables, int32_t max_blocks, int32_t num_blocks, const int32_t *__restrict__ free_blocks,
-    int32_t free_cap, const int32_t *free_count, int32_t *__restrict__ slot_mapping, int32_t *__restrict__ positions,
-    int32_t slots_cap, int32_t *__restrict__ cu_suffix, int32_t *context_lens, int32_t *free_count_out,
-    int32_t *__restrict__ status)
+struct AssignArgs {
+    const int32_t *prefix_lens, *suffix_lens, *free_blocks, *free_count;
+    int32_t *block_tables, *slot_mapping, *positions, *cu_suffix, *context_lens, *free_count_out, *status;
+    int32_t B, max_blocks, num_blocks, free_cap, slots_cap;
+    int32_t tile;                               // rows per workgroup
+    int32_t state;                              // the first workgroup writes the state
+};
+
+// Sequences in chunks of the workgroup's threads: each chunk's sums, then its rows of the tile.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void assign_kernel(const AssignArgs a)
 {
-    __shared__ uint32_t wave_sum[kWaves];
-    __shared__ int32_t first_bad;
-    __shared__ int32_t tok0[kThreads + 1];      // first token of each of the chunk's sequences
-    __shared__ int32_t prefix[kThreads];
-    __shared__ int32_t blk0[kThreads];          // blocks taken before each
+    __shared__ uint32_t wave_sum[2][THREADS / 64];
+    __shared__ int32_t wave_bad[THREADS / 64];  // first thread of each wave whose sequence does not fit
+    __shared__ int32_t tok[THREADS + 1];        // tokens, and blocks taken, before each of the chunk's sequences
+    __shared__ int32_t blk[THREADS + 1];
+    __shared__ int32_t prefix[THREADS];
     const int tid = threadIdx.x;
-    const int32_t count = min(max(*free_count, 0), free_cap);
-    uint32_t blocks = 0, tokens = 0;            // of the chunks so far
-    int32_t served = 0;
+    const bool state = a.state && blockIdx.x == 0;
+    const int32_t t_lo = (int32_t)min((int64_t)blockIdx.x * a.tile, (int64_t)a.slots_cap);
+    const int32_t t_hi = min(t_lo + a.tile, a.slots_cap);
+    const int32_t count = min(max(*a.free_count, 0), a.free_cap);
+    int32_t blocks = 0, tokens = 0, served = 0; // of the chunks so far
     bool open = true;                           // no sequence refused so far
-    if (tid == 0) cu_suffix[0] = 0;
-    for (int32_t b0 = 0; b0 < B; b0 += kThreads) {
-        const int32_t b = b0 + tid;
-        const int32_t p = b < B ? prefix_lens[b] : 0, s = b < B ? suffix_lens[b] : 0;
+    if (state && tid == 0) a.cu_suffix[0] = 0;
+    for (int32_t b0 = 0; b0 < a.B; b0 += THREADS) {
+        const int32_t b = b0 + tid, here = min(a.B - b0, THREADS);
+        const int32_t p = b < a.B ? a.prefix_lens[b] : 0, s = b < a.B ? a.suffix_lens[b] : 0;
         const bool lens_ok = p >= 0 && s >= 0;
         const int64_t held = lens_ok ? blocks_of(p) : 0, need = lens_ok ? blocks_of((int64_t)p + s) : 0;
-        uint32_t all_n, all_s;
-        const uint32_t nb = (uint32_t)(need - held);
-        const uint32_t incl_n = sat_add(blocks, block_scan(nb, wave_sum, &all_n));
-        const uint32_t incl_s = sat_add(tokens, block_scan(lens_ok ? (uint32_t)s : 0u, wave_sum, &all_s));
-        const bool fits = lens_ok && need <= max_blocks && incl_n <= (uint32_t)count && incl_s <= (uint32_t)slots_cap;
-        if (tid == 0) first_bad = open ? kThreads : 0;
-        __syncthreads();
-        if (!fits && b < B) atomicMin(&first_bad, tid);
-        __syncthreads();
-        const int n_seq = min(min(B - b0, kThreads), first_bad);   // served in this chunk
-        open = n_seq == min(B - b0, kThreads);
-        served += n_seq;
-        const bool mine = tid < n_seq;
-        if (mine) {
-            prefix[tid] = p;
-            tok0[tid + 1] = (int32_t)incl_s;
-            blk0[tid] = (int32_t)(incl_n - nb);
+        uint32_t sum[2] = {(uint32_t)(need - held), lens_ok ? (uint32_t)s : 0u};
+        block_scan<THREADS>(sum, wave_sum);
+        const uint32_t n = sat_add((uint32_t)blocks, sum[0]), t = sat_add((uint32_t)tokens, sum[1]);
+        const bool fits = b >= a.B || (lens_ok && need <= a.max_blocks && n <= (uint32_t)count && t <= (uint32_t)a.slots_cap);
+        const uint64_t bad = __builtin_amdgcn_ballot_w64(!fits);
+        if ((tid & 63) == 0) wave_bad[tid >> 6] = bad ? tid + (int)__builtin_ctzll(bad) : THREADS;
+        if (tid == 0) {
+            tok[0] = tokens;
+            blk[0] = blocks;
         }
-        if (tid == 0) tok0[0] = (int32_t)tokens;
+        tok[tid + 1] = (int32_t)t;
+        blk[tid + 1] = (int32_t)n;
+        prefix[tid] = p;
         __syncthreads();
-        const int32_t end = tok0[n_seq];
-        if (b < B) {
-            cu_suffix[b + 1] = mine ? (int32_t)incl_s : end;
-            context_lens[b] = mine ? p + s : p;
+        int n_seq = open ? here : 0;            // served in this chunk
+        for (int w = 0; w < THREADS / 64; ++w) n_seq = min(n_seq, wave_bad[w]);
+        open = n_seq == here;
+        const int32_t end = tok[n_seq];
+        if (state && b < a.B) {
+            a.cu_suffix[b + 1] = min(tok[tid + 1], end);
+            a.context_lens[b] = tid < n_seq ? p + s : p;
         }
-        for (int32_t t = tok0[0] + tid; t < end; t += kThreads) {
-            int lo = 0, hi = n_seq - 1;         // the last sequence that starts at or before t
+        for (int32_t r = max(t_lo, tokens) + tid; r < min(t_hi, end); r += THREADS) {
+            int lo = 0, hi = n_seq - 1;         // the last sequence that starts at or before r
             while (lo < hi) {
                 const int mid = (lo + hi + 1) / 2;
-                if (tok0[mid] <= t) lo = mid; else hi = mid - 1;
+                if (tok[mid] <= r) lo = mid; else hi = mid - 1;
             }
-            const int32_t pb = prefix[lo], pos = pb + (t - tok0[lo]);
+            const int32_t pb = prefix[lo], pos = pb + (r - tok[lo]);
             const int32_t entry = pos / kBlockSize, held_b = (int32_t)blocks_of(pb);
-            int32_t *row = block_tables + (int64_t)(b0 + lo) * max_blocks;
+            int32_t *row = a.block_tables + (int64_t)(b0 + lo) * a.max_blocks;
             int32_t id;
             if (entry < held_b) {
                 id = row[entry];
             } else {
-                id = free_blocks[count - 1 - (blk0[lo] + (entry - held_b))];
+                id = a.free_blocks[count - 1 - (blk[lo] + (entry - held_b))];
                 if (pos % kBlockSize == 0) row[entry] = id;
             }
-            slot_mapping[t] = id >= 0 && id < num_blocks ? id * kBlockSize + pos % kBlockSize : -1;
-            if (positions) positions[t] = pos;
+            a.slot_mapping[r] = id >= 0 && id < a.num_blocks ? id * kBlockSize + pos % kBlockSize : -1;
+            if (a.positions) a.positions[r] = pos;
         }
-        if (tid == n_seq - 1) wave_sum[0] = incl_n;   // blocks taken up to the last served one
-        __syncthreads();
-        if (n_seq) blocks = wave_sum[0];
-        tokens = (uint32_t)end;
-        __syncthreads();
+        tokens = end;
+        blocks = blk[n_seq];
+        served += n_seq;
+        __syncthreads();                        // the next chunk writes the arrays again
     }
-    for (int32_t t = (int32_t)tokens + tid; t < slots_cap; t += kThreads) {
-        slot_mapping[t] = -1;
-        if (positions) positions[t] = 0;
+    for (int32_t r = max(t_lo, tokens) + tid; r < t_hi; r += THREADS) {
+        a.slot_mapping[r] = -1;
+        if (a.positions) a.positions[r] = 0;
     }
-    if (tid == 0) {
-        *free_count_out = count - (int32_t)blocks;
-        status[0] = served;
-        status[1] = (int32_t)blocks;
-        status[2] = (int32_t)tokens;
+    if (state && tid == 0) {
+        *a.free_count_out = count - blocks;
+        a.status[0] = served;
+        a.status[1] = blocks;
+        a.status[2] = tokens;
     }
 }
 
-__device__ __forceinline__ void released(const int32_t *lens, const int32_t *keep_lens, int32_t b, int32_t B,
-                                         int32_t max_blocks, int32_t *first, uint32_t *n)
+struct ReleaseArgs {
+    const int32_t *lens, *keep_lens, *block_tables, *free_count;
+    int32_t *free_blocks, *free_count_out, *status;
+    int32_t B, max_blocks, free_cap;
+    int32_t tile;                               // ids per workgroup
+    int32_t state;                              // the first workgroup writes the state
+};
+
+// First entry that sequence b hands back, and how many.
+__device__ __forceinline__ void released(const ReleaseArgs &a, int32_t b, int32_t &first, uint32_t &n)
 {
-    *first = 0;
-    *n = 0;
-    if (b >= B) return;
-    const int64_t f = blocks_of(max(keep_lens[b], 0));
-    const int64_t l = blocks_of(min((int64_t)lens[b], (int64_t)max_blocks * kBlockSize));
-    *first = (int32_t)f;
-    *n = l > f ? (uint32_t)(l - f) : 0u;
+    first = 0;
+    n = 0;
+    if (b >= a.B) return;
+    const int64_t f = blocks_of(max(a.keep_lens[b], 0));
+    const int64_t l = blocks_of(min((int64_t)a.lens[b], (int64_t)a.max_blocks * kBlockSize));
+    first = (int32_t)f;
+    n = l > f ? (uint32_t)(l - f) : 0u;
 }
 
-__global__ __launch_bounds__(kThreads) void release_kernel(
-    int32_t B, const int32_t *__restrict__ lens, const int32_t *__restrict__ keep_lens,
-    const int32_t *__restrict__ block_tables, int32_t max_blocks, int32_t *__restrict__ free_blocks, int32_t free_cap,
-    const int32_t *free_count, int32_t *free_count_out, int32_t *__restrict__ status)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void release_kernel(const ReleaseArgs a)
 {
-    __shared__ uint32_t wave_sum[kWaves];
-    __shared__ uint32_t upto[kThreads];         // blocks up to and with each of the chunk's sequences
-    __shared__ int32_t first_e[kThreads];
+    __shared__ uint32_t wave_sum[1][THREADS / 64];
+    __shared__ uint32_t upto[THREADS + 1];      // ids of the chunk's sequences before each
+    __shared__ int32_t first_e[THREADS];
     const int tid = threadIdx.x;
-    const int32_t count = min(max(*free_count, 0), free_cap);
-    uint32_t total = 0;
-    for (int32_t b0 = 0; b0 < B; b0 += kThreads) {
-        int32_t f;
-        uint32_t n, all;
-        released(lens, keep_lens, b0 + tid, B, max_blocks, &f, &n);
-        (void)block_scan(n, wave_sum, &all);
-        total = sat_add(total, all);
-    }
-    const bool ok = total <= (uint32_t)(free_cap - count);
-    uint32_t before = 0;
-    for (int32_t b0 = 0; ok && b0 < B; b0 += kThreads) {
-        int32_t f;
-        uint32_t n, all;
-        released(lens, keep_lens, b0 + tid, B, max_blocks, &f, &n);
-        upto[tid] = block_scan(n, wave_sum, &all);
-        first_e[tid] = f;
+    const int32_t count = min(max(*a.free_count, 0), a.free_cap);
+    uint32_t total = 0, sum[1];
+    int32_t first = 0;
+    const bool once = a.B <= THREADS;           // one chunk: its sums serve both passes
+    for (int32_t b0 = 0; b0 < a.B; b0 += THREADS) {
+        released(a, b0 + tid, first, sum[0]);
+        block_scan<THREADS>(sum, wave_sum);
+        for (int w = 0; w < THREADS / 64; ++w) total = sat_add(total, wave_sum[0][w]);
         __syncthreads();
-        for (uint32_t k = tid; k < all; k += kThreads) {
-            int lo = 0, hi = kThreads - 1;      // the first sequence whose blocks reach beyond k
+    }
+    const bool ok = total <= (uint32_t)(a.free_cap - count);
+    const uint32_t k_lo = blockIdx.x * (uint32_t)a.tile;      // (k < 2^30: the grid ends with the free list)
+    const uint32_t k_hi = ok ? min(k_lo + (uint32_t)a.tile, total) : 0u;
+    uint32_t before = 0;
+    for (int32_t b0 = 0; b0 < a.B && before < k_hi; b0 += THREADS) {
+        if (!once) {
+            released(a, b0 + tid, first, sum[0]);
+            block_scan<THREADS>(sum, wave_sum);
+        }
+        if (tid == 0) upto[0] = before;
+        upto[tid + 1] = before + sum[0];        // (no saturation: below the total)
+        first_e[tid] = first;
+        __syncthreads();
+        const uint32_t end = upto[THREADS];
+        for (uint32_t k = max(k_lo, before) + tid; k < min(k_hi, end); k += THREADS) {
+            int lo = 0, hi = THREADS - 1;       // the first sequence whose ids reach beyond k
             while (lo < hi) {
                 const int mid = (lo + hi) / 2;
-                if (upto[mid] > k) hi = mid; else lo = mid + 1;
+                if (upto[mid + 1] > k) hi = mid; else lo = mid + 1;
             }
-            const uint32_t start = lo ? upto[lo - 1] : 0u;
-            const int32_t id = block_tables[(int64_t)(b0 + lo) * max_blocks + first_e[lo] + (int32_t)(k - start)];
-            free_blocks[count + (int64_t)total - 1 - (before + k)] = id;
+            a.free_blocks[count + (int64_t)total - 1 - k] =
+                a.block_tables[(int64_t)(b0 + lo) * a.max_blocks + first_e[lo] + (int32_t)(k - upto[lo])];
         }
-        before += all;
+        before = end;
         __syncthreads();
     }
-    if (tid == 0) {
-        *free_count_out = ok ? count + (int32_t)total : count;
-        status[0] = ok ? B : 0;
-        status[1] = ok ? (int32_t)total : 0;
-        status[2] = (int32_t)total;
+    if (a.state && blockIdx.x == 0 && tid == 0) {
+        *a.free_count_out = ok ? count + (int32_t)total : count;
+        a.status[0] = ok ? a.B : 0;
+        a.status[1] = ok ? (int32_t)total : 0;
+        a.status[2] = (int32_t)total;
     }
+}
+
+// Sequences up to which workgroups have 256 threads (a chunk of sequences each), 1024 above.
+constexpr int kBigBatch = 256;
+// Rows (ids) per thread where one workgroup takes them all for a state updated in place, at most
+// (500 rows of one sequence 3.2 us; a second launch adds about 2.5). Otherwise each thread
+// takes one: the rows' dependent loads are what a workgroup waits for (200 prompts in 131072 rows
+// 4.0 us, 4.7 with two rows a thread, 6.3 with four, 130 with one workgroup; 160 thousand released ids
+// of 500 rows 4.7, 5.4, 6.9 and 134; a decode step of 64 3.0).
+constexpr int kPerThread = 4;
+
+// One launch, or two where the state is updated in place and several workgroups read it.
+template <class Args>
+hipError_t launch_tiles(void (*small)(Args), void (*big)(Args), Args a, int64_t rows, bool in_place, hipStream_t s)
+{
+    const int threads = a.B <= kBigBatch ? 256 : 1024;
+    a.tile = in_place && rows <= threads * kPerThread ? threads * kPerThread : threads;
+    const int64_t wgs = rows > a.tile ? (rows + a.tile - 1) / a.tile : 1;
+    auto kernel = a.B <= kBigBatch ? small : big;
+    a.state = wgs == 1 || !in_place;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(threads), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.state) return e;
+    a.tile = 0;
+    a.state = 1;
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(threads), 0, s, a);
+    return hipGetLastError();
 }
 
 pcr_status check_tables(int32_t B, int32_t max_blocks, int32_t block_size, int32_t num_blocks, int32_t free_cap,
@@ -231,10 +280,11 @@ pcr_status pcr_assign_blocks(int32_t B, const int32_t *prefix_lens, const int32_
     if (!free_count || !cu_suffix || !free_count_out || !status || (slots_cap > 0 && !slot_mapping) ||
         (free_cap > 0 && !free_blocks) || (B > 0 && (!prefix_lens || !suffix_lens || !block_tables || !context_lens)))
         return fail(PCR_ERR_INVALID_ARG, "%s: NULL argument", who);
-    hipLaunchKernelGGL(assign_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), B, prefix_lens,
-                       suffix_lens, block_tables, max_blocks, num_blocks, free_blocks, free_cap, free_count,
-                       slot_mapping, positions, slots_cap, cu_suffix, context_lens, free_count_out, status);
-    const hipError_t e = hipGetLastError();
+    AssignArgs a{prefix_lens, suffix_lens, free_blocks, free_count, block_tables, slot_mapping, positions, cu_suffix,
+                 context_lens, free_count_out, status, B, max_blocks, num_blocks, free_cap, slots_cap, 0, 0};
+    const bool in_place = context_lens == prefix_lens || free_count_out == free_count;
+    const hipError_t e = launch_tiles(assign_kernel<256>, assign_kernel<1024>, a, slots_cap, in_place,
+                                      static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "pcr_assign_blocks: launch");
     return PCR_OK;
 }
@@ -251,9 +301,12 @@ pcr_status pcr_release_blocks(int32_t B, const int32_t *lens, const int32_t *kee
     if (!free_count || !free_count_out || !status || (free_cap > 0 && !free_blocks) ||
         (B > 0 && (!lens || !keep_lens || !block_tables)))
         return fail(PCR_ERR_INVALID_ARG, "%s: NULL argument", who);
-    hipLaunchKernelGGL(release_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), B, lens,
-                       keep_lens, block_tables, max_blocks, free_blocks, free_cap, free_count, free_count_out, status);
-    const hipError_t e = hipGetLastError();
+    ReleaseArgs a{lens, keep_lens, block_tables, free_count, free_blocks, free_count_out, status, B, max_blocks,
+                  free_cap, 0, 0};
+    // (no more ids than the rows hold, or than fit the stack)
+    const int64_t ids = (int64_t)B * max_blocks < free_cap ? (int64_t)B * max_blocks : free_cap;
+    const hipError_t e = launch_tiles(release_kernel<256>, release_kernel<1024>, a, ids, free_count_out == free_count,
+                                      static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "pcr_release_blocks: launch");
     return PCR_OK;
 }
