@@ -21,6 +21,11 @@
 // Row halves give each workgroup twice the work for one start-up and no merge; the
 // host takes them when they are estimated to be faster (schedule_time).
 //
+// Cross attention (CROSS; cross.hip) is the same work without the causal bound: every row of
+// a sequence attends its n keys, whatever the row. A sequence of up to 16 packed rows takes the
+// decode workgroup (all its columns see the same keys), and a key split leaves its partial
+// results in the caller's workspace. Sequences without keys are not part of the launch.
+//
 // Per wave and 64-key tile (4 pool blocks), with v_mfma_f32_32x32x16_bf16:
 //   S^T[key][q] = K Q^T   A = K rows from LDS, B = this wave's Q (registers)
 //   O^T[d][q]  += V^T P^T A = V^T from LDS,  B = P (registers)
@@ -50,6 +55,7 @@
 #include <algorithm>
 #include <atomic>
 #include <mutex>
+#include <new>
 #include <type_traits>
 #include <vector>
 
@@ -189,9 +195,10 @@ struct AttnWorkMap {
     int32_t per_head;                   // work items of all sequences, one kv head
     int32_t chunk;                      // key split: 64-key tiles per item (else unused)
     uint64_t launch;                    // key split: the launch's number (else unused)
+    char *workspace;                    // key split of cross attention: its partial results
     int32_t seq[kMaxMapSeqs];           // sequence in each slot
     int32_t tiles_end[kMaxMapSeqs];     // items of the slots up to and including this one
-    int32_t prefix[kMaxMapSeqs];        // the slot's cached tokens p
+    int32_t prefix[kMaxMapSeqs];        // the slot's cached tokens p (cross attention: its keys n)
     int32_t first[kMaxMapSeqs];         // the slot's first new token (row of q and out)
     int32_t count[kMaxMapSeqs];         // the slot's new tokens s
 };
@@ -233,6 +240,19 @@ __device__ SplitControl split_control;
 __device__ __attribute__((aligned(1024))) char split_o[kSplitSlots][kSplitParts][kSplitPartO];
 __device__ __attribute__((aligned(1024))) char split_ml[kSplitSlots][kSplitParts][kSplitPartML];
 
+// Partial results of part 0: in the library's scratch, or in the workspace of a cross attention
+// call (parts' O, then their maxima and sums).
+template <bool CROSS>
+__device__ __forceinline__ char *split_part_o(const AttnWorkMap &wm)
+{
+    return CROSS ? wm.workspace : &split_o[0][0][0];
+}
+template <bool CROSS>
+__device__ __forceinline__ char *split_part_ml(const AttnWorkMap &wm)
+{
+    return CROSS ? wm.workspace + (int64_t)kSplitParts * kSplitPartO : &split_ml[0][0][0];
+}
+
 // The entry owned by the launch with this number (wave-uniform), or -1. From kSplitSlots on
 // it has no scratch.
 __device__ __forceinline__ int split_entry(uint64_t launch)
@@ -259,11 +279,12 @@ __device__ __host__ __forceinline__ int key_tiles(int last) { return last / kTil
 // units.
 // Keys [n0, n_keys) of the row; with part_o they leave the unnormalised O, max and sum
 // there (a chunk of a key-split launch), otherwise the row is written.
-template <int D>
+// CROSS: the columns are the packed rows of `s` tokens.
+template <int D, bool CROSS>
 __device__ __forceinline__ void decode_workgroup(const u16 *__restrict__ q, const u16 *__restrict__ pool_k,
                                                  const u16 *__restrict__ pool_v, int32_t num_blocks, int32_t Hkv,
                                                  const int32_t *__restrict__ bt_row, int32_t max_blocks, int g, int G,
-                                                 int32_t Hq, int n0, int n_keys, int64_t t0, float scale_log2,
+                                                 int32_t Hq, int n0, int n_keys, int64_t t0, int s, float scale_log2,
                                                  u16 *__restrict__ out, char *lds, f32x4 *part_out,
                                                  float *part_out_ml)
 {
@@ -277,8 +298,9 @@ __device__ __forceinline__ void decode_workgroup(const u16 *__restrict__ q, cons
     const int kend = min(n_keys, kbeg + chunk);
     const int last_blk = max(0, min((n_keys - 1) >> 4, max_blocks - 1));
     const int c = lane & 15, q4 = lane >> 4;
-    const bool col = c < G;
-    const int h = g * G + c;
+    const bool col = c < (CROSS ? s * G : G);
+    const int h = g * G + (CROSS ? c % G : c);
+    if constexpr (CROSS) t0 += col ? c / G : 0;
     f32x4 o[MT];
     float m_run = decode_wave::kNoMax, l_run = 0.f;
     if (kbeg < n_keys) {
@@ -420,7 +442,14 @@ __device__ __forceinline__ void store_rows(const char *stage, int lane, int orow
     }
 }
 
-template <int D, int MODE>
+// A sequence whose rows one decode workgroup takes.
+template <bool CROSS>
+__device__ __host__ __forceinline__ bool few_rows(int s, int G)
+{
+    return CROSS ? s * G <= decode_wave::kMaxCols : s == 1 && G <= decode_wave::kMaxCols;
+}
+
+template <int D, int MODE, bool CROSS>
 __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const u16 *__restrict__ q, const u16 *__restrict__ pool_k, const u16 *__restrict__ pool_v,
     int32_t num_blocks, int32_t Hkv, const int32_t *__restrict__ block_tables, int32_t max_blocks, int32_t Hq,
@@ -450,10 +479,10 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     // Key split: item `local` of the sequence is chunk sp of row tile rt.
     int rt = it.local, sp = 0, part = -1;
     if constexpr (MODE == kKeySplit) {
-        const int ns = (key_tiles(p + s - 1) + wm.chunk - 1) / wm.chunk;
+        const int ns = (key_tiles(CROSS ? p - 1 : p + s - 1) + wm.chunk - 1) / wm.chunk;
         rt = it.local / ns;
         sp = it.local - rt * ns;
-        const int slot = split_entry(wm.launch);
+        const int slot = CROSS ? 0 : split_entry(wm.launch);
         const bool whole = slot < 0 || slot >= kSplitSlots;
         if (whole && sp > 0) return;                 // unsplit: chunk 0 takes every key
         if (!whole) part = slot * kSplitParts + g * wm.per_head + it.j;
@@ -467,25 +496,25 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const int rows_total = s * G;
     const int row0 = rt * RPW;
     if (s <= 0 || row0 >= rows_total || T <= 0) return;   // uniform over the workgroup
-    if (s == 1 && G <= decode_wave::kMaxCols) {           // a decode row (uniform too)
+    if (few_rows<CROSS>(s, G)) {                          // a decode row (uniform too)
         static_assert(kThreads / 64 * (D / 16) * 64 * 16 + kThreads / 64 * 64 * 8 <= (int)sizeof(lds), "merge area");
         if (t0 >= T) return;
-        int n0 = 0, n_keys = p + 1;                  // keys 0 .. p: the row's causal range
+        int n0 = 0, n_keys = CROSS ? p : p + 1;      // keys 0 .. p: the row's causal range
         f32x4 *po = nullptr;
         float *pml = nullptr;
         if constexpr (MODE == kKeySplit) {
             if (part >= 0 && n_keys > wm.chunk * kTileKeys) {
                 n0 = sp * wm.chunk * kTileKeys;
                 n_keys = min(n_keys, n0 + wm.chunk * kTileKeys);
-                po = reinterpret_cast<f32x4 *>(&split_o[0][0][0] + (int64_t)part * kSplitPartO);
-                pml = reinterpret_cast<float *>(&split_ml[0][0][0] + (int64_t)part * kSplitPartML);
+                po = reinterpret_cast<f32x4 *>(split_part_o<CROSS>(wm) + (int64_t)part * kSplitPartO);
+                pml = reinterpret_cast<float *>(split_part_ml<CROSS>(wm) + (int64_t)part * kSplitPartML);
             }
         }
-        decode_workgroup<D>(q, pool_k, pool_v, num_blocks, Hkv, block_tables + (int64_t)b * max_blocks, max_blocks,
-                            g, G, Hq, n0, n_keys, t0, scale_log2, out, &lds[0][0], po, pml);
+        decode_workgroup<D, CROSS>(q, pool_k, pool_v, num_blocks, Hkv, block_tables + (int64_t)b * max_blocks,
+                                   max_blocks, g, G, Hq, n0, n_keys, t0, s, scale_log2, out, &lds[0][0], po, pml);
         return;
     }
-    const int total = p + s;
+    const int total = CROSS ? p : p + s;
 
     // This lane's packed query row (rows past the end compute a copy of the last row).
     const int wrow0 = row0 + (ROWS ? grp * kRowsPerWG : 0) + wg * kRowsPerWave;   // this wave's first row
@@ -493,7 +522,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const bool row_valid = R < rows_total;
     const int Rc = row_valid ? R : rows_total - 1;
     const int i = Rc / G, hl = Rc - i * G;
-    const int limit = p + i;                         // last key this row attends to
+    const int limit = CROSS ? p - 1 : p + i;         // last key this row attends to
     const int tq = min(t0 + i, T - 1);               // (T * Hq fits 31 bits)
     const int qrow = tq * Hq + g * G + hl;           // its row of q and out
     // Its output row, -1 past the end; held in one register over the loop.
@@ -501,7 +530,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     asm volatile("" : "+v"(orow));
 
     const int wg_last = min(rows_total - 1, row0 + RPW - 1);
-    const int all_tiles = key_tiles(p + wg_last / G);
+    const int all_tiles = key_tiles(CROSS ? p - 1 : p + wg_last / G);
     // This workgroup's tiles [t_lo, t_lo + ntiles): all, or a chunk of a key split.
     int t_lo = 0, ntiles = all_tiles;
     if constexpr (MODE == kKeySplit) {
@@ -518,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const int tile_begin = t_lo + ((!ROWS && grp) ? split : 0);
     const int n = (ROWS || !grp) ? split : ntiles - split;        // this group's tiles
     const int w_first = min(rows_total - 1, wrow0);
-    const int w_min_limit = p + w_first / G;
+    const int w_min_limit = CROSS ? p - 1 : p + w_first / G;
     const int valid_blocks = min((total + kBlockSize - 1) / kBlockSize, max_blocks);
 
     bf16x8 qf[KSTEPS];    // the Q^T operand (k-step ks: dims 16ks + 8half .. +7 of this lane's row)
@@ -998,9 +1027,9 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         if (part >= 0) {
             // A chunk's partial result, in the lane layout (1 KB per wave-wide store).
             if (orow >= 0) {
-                f32x4 *po = reinterpret_cast<f32x4 *>(&split_o[0][0][0] + (int64_t)part * kSplitPartO) +
+                f32x4 *po = reinterpret_cast<f32x4 *>(split_part_o<CROSS>(wm) + (int64_t)part * kSplitPartO) +
                             wg * MT * 4 * 64 + lane;
-                f32x2 *pml = reinterpret_cast<f32x2 *>(&split_ml[0][0][0] + (int64_t)part * kSplitPartML) +
+                f32x2 *pml = reinterpret_cast<f32x2 *>(split_part_ml<CROSS>(wm) + (int64_t)part * kSplitPartML) +
                              wg * 64 + lane;
 #pragma unroll
                 for (int k = 0; k < MH; ++k)
@@ -1129,14 +1158,14 @@ __global__ __launch_bounds__(64) void split_release_kernel(uint64_t launch, unsi
 // dims) are dealt to the waves of all its chunks' workgroups, so the reads of the
 // partial results, which bound this kernel, come from every compute unit.
 constexpr int kCombineThreads = 512;
-template <int D>
+template <int D, bool CROSS>
 __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t Hkv, int32_t Hq, int32_t T,
                                                                         float scale_log2, u16 *__restrict__ out,
                                                                         const AttnWorkMap wm)
 {
     constexpr int MT = D / 32;
     constexpr int kCombineWaves = kCombineThreads / 64;
-    const int slot = split_entry(wm.launch);
+    const int slot = CROSS ? 0 : split_entry(wm.launch);
     if (slot < 0) return;                            // ran unsplit
     const Item it = locate_item(wm, Hkv);
     const int lane = threadIdx.x & 63;
@@ -1144,16 +1173,17 @@ __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t 
     const int G = Hq / Hkv;
     if (it.g < Hkv && slot < kSplitSlots) {          // (past them: ran unsplit, counts itself out)
         const int p = it.p, s = it.s, rows_total = s * G;
-        const int ns_seq = (key_tiles(p + s - 1) + wm.chunk - 1) / wm.chunk;
+        const int ns_seq = (key_tiles(CROSS ? p - 1 : p + s - 1) + wm.chunk - 1) / wm.chunk;
         const int rt = it.local / ns_seq, sp = it.local - rt * ns_seq;
         const int row0 = rt * kRowsPerWG;
-        const bool decode_row = s == 1 && G <= decode_wave::kMaxCols;
+        const bool decode_row = few_rows<CROSS>(s, G);
         const int wg_last = min(rows_total - 1, row0 + kRowsPerWG - 1);
-        const int ns = (key_tiles(p + wg_last / G) + wm.chunk - 1) / wm.chunk;   // chunks of this row tile
+        const int ns =                                        // chunks of this row tile
+            (key_tiles(CROSS ? p - 1 : p + wg_last / G) + wm.chunk - 1) / wm.chunk;
         // chunk s of the row tile is item j + sp - s (items count down)
         const int64_t part0 = (int64_t)slot * kSplitParts + it.g * wm.per_head + it.j + sp;
-        const f32x4 *po = reinterpret_cast<const f32x4 *>(&split_o[0][0][0]);
-        const f32x2 *pml = reinterpret_cast<const f32x2 *>(&split_ml[0][0][0]);
+        const f32x4 *po = reinterpret_cast<const f32x4 *>(split_part_o<CROSS>(wm));
+        const f32x2 *pml = reinterpret_cast<const f32x2 *>(split_part_ml<CROSS>(wm));
         const int waves = (wg_last - row0) / kRowsPerWave + 1;   // of the row tile, with rows
         const int pieces = ns <= 1 || row0 >= rows_total ? 0 : decode_row ? D / 16 : waves * MT * 4;
         const float c = decode_row ? 1.f : scale_log2;    // a decode row's max is scaled already
@@ -1163,10 +1193,11 @@ __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t 
             int h, d0;
             bool ok;
             if (decode_row) {                        // piece = 16 dims; lane = head lane % 16, dims 4 (lane / 16) ..
-                h = it.g * G + (lane & 15);
-                tq = it.t0;
+                const int col = lane & 15;
+                h = it.g * G + (CROSS ? col % G : col);
+                tq = CROSS ? (int64_t)it.t0 + col / G : it.t0;
                 d0 = 16 * pc + 4 * (lane >> 4);
-                ok = (lane & 15) < G;
+                ok = col < (CROSS ? s * G : G);
             } else {                                 // piece = (wave, 8 dims); lane = row lane % 32, half lane / 32
                 const int R = row0 + wg * kRowsPerWave + (lane & 31);
                 const int kr = pc - wg * MT * 4;
@@ -1215,6 +1246,7 @@ __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t 
             *reinterpret_cast<u32x2 *>(out + (tq * Hq + h) * D + d0) = __builtin_bit_cast(u32x2, bv);
         }
     }
+    if constexpr (CROSS) return;                     // (the workspace is the caller's)
     // This workgroup is through with the slot: it only reads it, and every read has returned
     // its value before the barrier.
     __syncthreads();
@@ -1248,12 +1280,24 @@ hipError_t enqueue(void (*kernel)(P...), dim3 grid, int threads, hipStream_t s, 
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), args, 0, s);
 }
 
-template <int D, int MODE>
+// A launch's sequences: which keys their rows see.
+struct Seqs {
+    const int32_t *keys;      // cached tokens p (causal), or all keys n (cross attention)
+    const int32_t *cu;        // rows
+    bool cross;
+    int G;
+    int32_t rows(int32_t b) const { return cu[b + 1] - cu[b]; }
+    // last key of row i of sequence b
+    int32_t last(int32_t b, int32_t i) const { return cross ? keys[b] - 1 : keys[b] + i; }
+    bool few(int32_t b) const { return cross ? few_rows<true>(rows(b), G) : few_rows<false>(rows(b), G); }
+};
+
+template <int D, int MODE, bool CROSS>
 void launch_attn(dim3 grid, hipStream_t s, const u16 *qq, const u16 *pk, const u16 *pv, const pcr_kv_pool &pool,
                  const int32_t *block_tables, int32_t max_blocks, int32_t num_q_heads, int32_t T, float scale_log2,
                  float rescale_thr, u16 *oo, const AttnWorkMap &wm)
 {
-    hipLaunchKernelGGL((prefill_attn_kernel<D, MODE>), grid, dim3(kThreads), 0, s, qq, pk, pv, pool.num_blocks,
+    hipLaunchKernelGGL((prefill_attn_kernel<D, MODE, CROSS>), grid, dim3(kThreads), 0, s, qq, pk, pv, pool.num_blocks,
                        pool.num_kv_heads, block_tables, max_blocks, num_q_heads, T, scale_log2, rescale_thr, oo,
                        wm);
 }
@@ -1277,22 +1321,21 @@ void launch_attn(dim3 grid, hipStream_t s, const u16 *qq, const u16 *pk, const u
 // chunk as the line, whatever the rows and dims, had 73 slower ones, up to 57% (a decode
 // row of 64 dims on 1250 keys). (Chunks of at least 4, 6, 8, 12 or 16 tiles: 4 to 8 alike, 12
 // and 16 up to 20% slower on prefixes of 2k.)
-int32_t split_chunk(const int32_t *seq, int n, const int32_t *host_prefix_lens, const int32_t *host_cu_suffix, int G,
-                    int Hkv, int D, int n_cu)
+int32_t split_chunk(const int32_t *seq, int n, const Seqs &q, int Hkv, int D, int n_cu)
 {
     const int64_t cap = std::min(n_cu, kSplitParts);
     int32_t longest[2] = {0, 0};             // key tiles: of the row tiles, of the decode rows
     for (int k = 0; k < n; ++k) {
-        const int32_t b = seq[k], sb = host_cu_suffix[b + 1] - host_cu_suffix[b];
-        int32_t &l = longest[sb == 1 && G <= decode_wave::kMaxCols];
-        l = std::max(l, key_tiles(host_prefix_lens[b] + sb - 1));
+        const int32_t b = seq[k];
+        int32_t &l = longest[q.few(b)];
+        l = std::max(l, key_tiles(q.last(b, q.rows(b) - 1)));
     }
     auto items = [&](int32_t c) {            // of chunks of c tiles (0: whole)
         int64_t w = 0;
         for (int k = 0; k < n; ++k) {
-            const int32_t b = seq[k], sb = host_cu_suffix[b + 1] - host_cu_suffix[b];
-            w += ((int64_t)sb * G + kRowsPerWG - 1) / kRowsPerWG *
-                 (c ? (key_tiles(host_prefix_lens[b] + sb - 1) + c - 1) / c : 1);
+            const int32_t b = seq[k], sb = q.rows(b);
+            w += ((int64_t)sb * q.G + kRowsPerWG - 1) / kRowsPerWG *
+                 (c ? (key_tiles(q.last(b, sb - 1)) + c - 1) / c : 1);
         }
         return w * Hkv;
     };
@@ -1332,8 +1375,7 @@ int32_t split_chunk(const int32_t *seq, int n, const int32_t *host_prefix_lens, 
 // an estimate from the items' mean lost up to 11% against that line in 29 of them, and
 // 30% on two sequences of 2100 new tokens on 90 cached with 28 / 4 heads (103 -> 79 us).
 constexpr int kSimItems = 1024;
-double schedule_time(const int32_t *order, int n, const int32_t *host_prefix_lens, const int32_t *host_cu_suffix,
-                     int G, int Hkv, int D, int rpw, int n_cu, bool simulate)
+double schedule_time(const int32_t *order, int n, const Seqs &q, int Hkv, int D, int rpw, int n_cu, bool simulate)
 {
     const bool rows = rpw > kRowsPerWG, wide = D == 128;
     const float fixed = rows ? (wide ? 10.f : 7.6f) : (wide ? 7.3f : 5.6f);
@@ -1343,21 +1385,23 @@ double schedule_time(const int32_t *order, int n, const int32_t *host_prefix_len
     int items = 0;
     double total = 0.0;
     for (int k = 0; k < n; ++k) {
-        const int32_t b = order[k], p = host_prefix_lens[b], sb = host_cu_suffix[b + 1] - host_cu_suffix[b];
-        if (sb == 1 && G <= decode_wave::kMaxCols) {
-            const float t = dec_fixed + dec_tile * key_tiles(p);
+        const int32_t b = order[k], sb = q.rows(b);
+        if (q.few(b)) {
+            const float t = dec_fixed + dec_tile * key_tiles(q.last(b, 0));
             total += t;
             if (simulate) cost[items++] = t;
             continue;
         }
-        const int64_t r = (int64_t)sb * G, nt = (r + rpw - 1) / rpw;
+        const int64_t r = (int64_t)sb * q.G, nt = (r + rpw - 1) / rpw;
         if (!simulate) {
-            const int first = key_tiles(p + (int)((std::min<int64_t>(r, rpw) - 1) / G)), last = key_tiles(p + sb - 1);
+            const int first = key_tiles(q.last(b, (int)((std::min<int64_t>(r, rpw) - 1) / q.G)));
+            const int last = key_tiles(q.last(b, sb - 1));
             total += nt * (fixed + tile * 0.5 * (first + last));
             continue;
         }
         for (int64_t t = nt - 1; t >= 0; --t) {
-            cost[items++] = fixed + tile * key_tiles(p + (int)((std::min<int64_t>(r, (t + 1) * rpw) - 1) / G));
+            cost[items++] =
+                fixed + tile * key_tiles(q.last(b, (int)((std::min<int64_t>(r, (t + 1) * rpw) - 1) / q.G)));
         }
     }
     if (!simulate) return total * Hkv / n_cu;
@@ -1391,14 +1435,18 @@ double schedule_time(const int32_t *order, int n, const int32_t *host_prefix_len
 }
 
 // One launch over the sequences seq[0..n) (each with new tokens, n <= kMaxMapSeqs,
-// longest context first): builds the work map, picks the schedule, launches.
+// longest context first): builds the work map, picks the schedule, launches. split_ws: of
+// cross attention, the workspace of a key split.
+template <bool CROSS>
 hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_pool &pool,
                         const int32_t *block_tables, int32_t max_blocks, const int32_t *host_prefix_lens,
                         const int32_t *host_cu_suffix, int32_t num_q_heads, int32_t T, float scale_log2,
-                        float rescale_thr, u16 *oo, hipStream_t s, int auto_schedule, int n_cu, bool can_split)
+                        float rescale_thr, u16 *oo, hipStream_t s, int auto_schedule, int n_cu, bool can_split,
+                        void *split_ws)
 {
     const int Hkv = pool.num_kv_heads, G = num_q_heads / Hkv;
-    auto rows_of = [&](int32_t b) { return ((int64_t)host_cu_suffix[b + 1] - host_cu_suffix[b]) * G; };
+    const Seqs sq{host_prefix_lens, host_cu_suffix, CROSS, G};
+    auto rows_of = [&](int32_t b) { return (int64_t)sq.rows(b) * G; };
     const int sched = g_schedule.load(std::memory_order_relaxed);
     const bool prefer_keys = auto_schedule == PCR_ATTN_SCHEDULE_KEY_HALVES;
     // Slot order: the given order (longest context first), with the decode rows (one
@@ -1406,12 +1454,11 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     // tiles (bound by the matrix cores): run back to back they would take every
     // compute unit at once and queue on HBM.
     auto slot_order = [&](auto tiles_of, int32_t *order) {
-        const bool dec_rows = G <= decode_wave::kMaxCols;
         int32_t pre[kMaxMapSeqs], dec[kMaxMapSeqs];
         int np = 0, nd = 0;
         int64_t pre_tiles = 0;
         for (int k = 0; k < n; ++k) {
-            if (dec_rows && rows_of(seq[k]) == G) {
+            if (sq.few(seq[k])) {
                 dec[nd++] = seq[k];
             } else {
                 pre[np++] = seq[k];
@@ -1452,8 +1499,7 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
             auto time_of = [&](int rpw) {
                 int32_t order[kMaxMapSeqs];
                 slot_order([&](int32_t b) { return (rows_of(b) + rpw - 1) / rpw; }, order);
-                return schedule_time(order, n, host_prefix_lens, host_cu_suffix, G, Hkv, pool.head_dim, rpw, n_cu,
-                                     simulate);
+                return schedule_time(order, n, sq, Hkv, pool.head_dim, rpw, n_cu, simulate);
             };
             const bool line = tiles2 >= 2 * (int64_t)n_cu;
             rows = time_of(2 * kRowsPerWG) < (line ? 1.04 : 0.96) * time_of(kRowsPerWG);
@@ -1463,12 +1509,11 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     // Key tiles per item, 0: no key split.
     const int32_t chunk =
         sched == PCR_ATTN_SCHEDULE_AUTO && !prefer_keys && !rows && can_split
-            ? split_chunk(seq, n, host_prefix_lens, host_cu_suffix, G, Hkv, pool.head_dim, n_cu)
+            ? split_chunk(seq, n, sq, Hkv, pool.head_dim, n_cu)
             : 0;
-    auto keys_of = [&](int32_t b) { return host_prefix_lens[b] + host_cu_suffix[b + 1] - host_cu_suffix[b]; };
     auto tiles_of = [&](int32_t b) {
         const int64_t t = (rows_of(b) + rpw - 1) / rpw;
-        return chunk ? t * ((key_tiles(keys_of(b) - 1) + chunk - 1) / chunk) : t;
+        return chunk ? t * ((key_tiles(sq.last(b, sq.rows(b) - 1)) + chunk - 1) / chunk) : t;
     };
 
     AttnWorkMap wm;
@@ -1485,7 +1530,8 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     wm.n_seq = n;
     wm.per_head = cum;
     wm.chunk = chunk;
-    wm.launch = chunk ? next_launch() : 0;
+    wm.launch = chunk && !CROSS ? next_launch() : 0;
+    wm.workspace = static_cast<char *>(split_ws);
     const int64_t n_items = (Hkv % kXcds == 0) ? (int64_t)cum * Hkv : ((int64_t)cum * Hkv + kXcds - 1) / kXcds * kXcds;
     const dim3 grid((unsigned)n_items);
     auto *pk = static_cast<const u16 *>(pool.k);
@@ -1493,13 +1539,20 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     auto launch = [&](auto dim) -> hipError_t {
         constexpr int D = decltype(dim)::value;
         auto attn = [&](auto mode) {
-            launch_attn<D, decltype(mode)::value>(grid, s, qq, pk, pv, pool, block_tables, max_blocks, num_q_heads,
-                                                  T, scale_log2, rescale_thr, oo, wm);
+            launch_attn<D, decltype(mode)::value, CROSS>(grid, s, qq, pk, pv, pool, block_tables, max_blocks, num_q_heads,
+                                                         T, scale_log2, rescale_thr, oo, wm);
         };
         if (rows) {
             attn(std::integral_constant<int, kRowHalves>{});
         } else if (!chunk) {
             attn(std::integral_constant<int, kKeyHalves>{});
+        } else if constexpr (CROSS) {
+            hipError_t e = enqueue(prefill_attn_kernel<D, kKeySplit, true>, grid, kThreads, s, qq, pk, pv, pool.num_blocks,
+                                   Hkv, block_tables, max_blocks, num_q_heads, T, scale_log2, rescale_thr, oo, wm);
+            if (e == hipSuccess)
+                e = enqueue(split_combine_kernel<D, true>, grid, kCombineThreads, s, Hkv, num_q_heads, T, scale_log2,
+                            oo, wm);
+            return e;
         } else {
             // (the grid is a multiple of the XCD count) A claim without its combine kernel
             // would hold its slot for good.
@@ -1510,10 +1563,10 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
             e = enqueue(capture == hipStreamCaptureStatusNone ? split_claim_kernel : split_claim_replay_kernel,
                         dim3(1), 64, s, wm.launch, per_xcd);
             if (e != hipSuccess) return e;
-            e = enqueue(prefill_attn_kernel<D, kKeySplit>, grid, kThreads, s, qq, pk, pv, pool.num_blocks, Hkv,
+            e = enqueue(prefill_attn_kernel<D, kKeySplit, false>, grid, kThreads, s, qq, pk, pv, pool.num_blocks, Hkv,
                         block_tables, max_blocks, num_q_heads, T, scale_log2, rescale_thr, oo, wm);
             if (e == hipSuccess)
-                e = enqueue(split_combine_kernel<D>, grid, kCombineThreads, s, Hkv, num_q_heads, T, scale_log2, oo,
+                e = enqueue(split_combine_kernel<D, false>, grid, kCombineThreads, s, Hkv, num_q_heads, T, scale_log2, oo,
                             wm);
             if (e != hipSuccess) {
                 (void)enqueue(split_release_kernel, dim3(1), 64, s, wm.launch, per_xcd);
@@ -1568,20 +1621,21 @@ hipError_t attn_hold_scratch(int n, int *free_entries)
     return hipSuccess;
 }
 
-hipError_t launch_prefix_prefill_attn(const void *q, const pcr_kv_pool &pool,
-                                      const int32_t *block_tables, int32_t max_blocks,
-                                      const int32_t *host_prefix_lens, const int32_t *host_cu_suffix,
-                                      int32_t B, int32_t num_q_heads, int32_t T, float sm_scale, void *out,
-                                      hipStream_t s, int auto_schedule, int n_cu)
+namespace {
+// The sequences with rows, longest context first, in as many launches as the work map takes.
+template <bool CROSS>
+hipError_t launch_batch(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
+                        const int32_t *keys, const int32_t *cu, int32_t B, int32_t num_q_heads, int32_t T,
+                        float sm_scale, void *out, hipStream_t s, int auto_schedule, int n_cu, bool can_split,
+                        void *split_ws)
 {
-    // The sequences with new tokens, longest context first.
     std::vector<int32_t> seq;
     seq.reserve((size_t)std::max(B, 0));
     for (int32_t b = 0; b < B; ++b)
-        if (host_cu_suffix[b + 1] > host_cu_suffix[b]) seq.push_back(b);
+        if (cu[b + 1] > cu[b] && (!CROSS || keys[b] > 0)) seq.push_back(b);
     if (seq.empty()) return hipSuccess;
-    auto keys = [&](int32_t b) { return (int64_t)host_prefix_lens[b] + host_cu_suffix[b + 1] - host_cu_suffix[b]; };
-    std::stable_sort(seq.begin(), seq.end(), [&](int32_t a, int32_t c) { return keys(a) > keys(c); });
+    auto context = [&](int32_t b) { return CROSS ? (int64_t)keys[b] : (int64_t)keys[b] + cu[b + 1] - cu[b]; };
+    std::stable_sort(seq.begin(), seq.end(), [&](int32_t a, int32_t c) { return context(a) > context(c); });
     const float scale_log2 = sm_scale * kLog2e;
     const float rescale_thr = kRescaleThreshold / scale_log2;   // in units of <q,k>
     auto *qq = static_cast<const u16 *>(q);
@@ -1592,20 +1646,44 @@ hipError_t launch_prefix_prefill_attn(const void *q, const pcr_kv_pool &pool,
     const int n_act = (int)seq.size();
     const int n_launch = (n_act + kMaxMapSeqs - 1) / kMaxMapSeqs;
     int32_t group[kMaxMapSeqs];
+    for (int l = 0; l < n_launch; ++l) {
+        int n = 0;
+        for (int k = l; k < n_act; k += n_launch) group[n++] = seq[k];
+        const hipError_t e =
+            launch_group<CROSS>(group, n, qq, pool, block_tables, max_blocks, keys, cu, num_q_heads, T, scale_log2,
+                                rescale_thr, oo, s, auto_schedule, n_cu, can_split && n_launch == 1, split_ws);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+}  // namespace
+
+hipError_t launch_prefix_prefill_attn(const void *q, const pcr_kv_pool &pool,
+                                      const int32_t *block_tables, int32_t max_blocks,
+                                      const int32_t *host_prefix_lens, const int32_t *host_cu_suffix,
+                                      int32_t B, int32_t num_q_heads, int32_t T, float sm_scale, void *out,
+                                      hipStream_t s, int auto_schedule, int n_cu)
+{
     // A key-split launch's chunks read q until its combine kernel writes out, and its rows
     // that need no merge are written beside them: not for outputs that overlap q.
     const uintptr_t qa = (uintptr_t)q, oa = (uintptr_t)out;
     const uintptr_t bytes = (uintptr_t)T * num_q_heads * pool.head_dim * 2;
-    const bool can_split = n_launch == 1 && (qa + bytes <= oa || oa + bytes <= qa);
-    for (int l = 0; l < n_launch; ++l) {
-        int n = 0;
-        for (int k = l; k < n_act; k += n_launch) group[n++] = seq[k];
-        const hipError_t e = launch_group(group, n, qq, pool, block_tables, max_blocks, host_prefix_lens,
-                                          host_cu_suffix, num_q_heads, T, scale_log2, rescale_thr, oo, s,
-                                          auto_schedule, n_cu, can_split);
-        if (e != hipSuccess) return e;
+    return launch_batch<false>(q, pool, block_tables, max_blocks, host_prefix_lens, host_cu_suffix, B, num_q_heads, T,
+                               sm_scale, out, s, auto_schedule, n_cu, qa + bytes <= oa || oa + bytes <= qa, nullptr);
+}
+
+int64_t cross_tiles_workspace_bytes() { return (int64_t)kSplitParts * (kSplitPartO + kSplitPartML); }
+
+hipError_t launch_cross_tiles(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
+                              const int32_t *host_key_lens, const int32_t *host_cu_q, int32_t B, int32_t num_q_heads,
+                              int32_t T, float sm_scale, void *out, void *workspace, hipStream_t s, int n_cu)
+{
+    try {
+        return launch_batch<true>(q, pool, block_tables, max_blocks, host_key_lens, host_cu_q, B, num_q_heads, T,
+                                  sm_scale, out, s, PCR_ATTN_SCHEDULE_AUTO, n_cu, workspace != nullptr, workspace);
+    } catch (const std::bad_alloc &) {       // (the list of sequences)
+        return hipErrorOutOfMemory;
     }
-    return hipSuccess;
 }
 
 }  // namespace pcr

@@ -3,59 +3,43 @@
 // the paged pool through the block table.
 //
 // The s * G query rows of one (sequence, kv head) see the same keys, so they are packed
-// (row r = token r / G, head-in-group r % G). A wave takes 16 packed rows as the columns of
-// the decode routine's tiles (decode_wave.h) and walks all keys.
-#include "decode_wave.h"
+// (row r = token r / G, head-in-group r % G). A batch whose sequences have up to 16 packed rows
+// each (decode steps, beams) is bound by reading K and V: it runs on the decode kernels
+// (decode.hip), whose waves hold the packed rows as the columns of one matrix tile and cut the
+// keys among them. Any other runs on the row tiles of the prefill kernel (attn.hip) without
+// their causal bound; its sequences of few rows take a decode workgroup in the same launch,
+// those without keys a kernel that writes their zeros.
+#include <algorithm>
+
 #include "pcr_internal.h"
 
 namespace pcr {
 namespace {
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short u16;
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kCols = decode_wave::kMaxCols;
-
-// Grid (row tiles of the longest sequence, Hkv, B), one wave.
-template <int D>
-__global__ __launch_bounds__(64) void cross_kernel(const u16 *__restrict__ q, const u16 *__restrict__ pool_k,
-                                                   const u16 *__restrict__ pool_v, int32_t num_blocks, int32_t Hkv,
-                                                   const int32_t *__restrict__ block_tables, int32_t max_blocks,
-                                                   const int32_t *__restrict__ key_lens,
-                                                   const int32_t *__restrict__ cu_q, int32_t T, int32_t Hq,
-                                                   float scale_log2, u16 *__restrict__ out)
+// Zero rows of the sequences without keys, beside a launch of row tiles. Grid (B, slices).
+constexpr int kZeroThreads = 256;
+constexpr int64_t kZeroSlice = 64 << 10;    // bytes of the longest such sequence per workgroup
+__global__ __launch_bounds__(kZeroThreads) void cross_zero_kernel(const int32_t *__restrict__ key_lens,
+                                                                  const int32_t *__restrict__ cu_q, int32_t T,
+                                                                  int64_t row_vecs, u32x4 *__restrict__ out)
 {
-    constexpr int MT = D / 16;
-    const int lane = threadIdx.x, c = lane & 15, q4 = lane >> 4;
-    const int g = blockIdx.y, b = blockIdx.z, G = Hq / Hkv;
-    const int t0 = cu_q[b], t1 = min(cu_q[b + 1], T);
-    const int64_t rows = (int64_t)(t1 - t0) * G, row0 = (int64_t)blockIdx.x * kCols;
-    if (t0 < 0 || row0 >= rows) return;
-    const bool col = row0 + c < rows;
-    const int64_t r = col ? row0 + c : row0;
-    const int64_t qrow = (t0 + r / G) * Hq + g * G + r % G;
-    const int n = (int)min((int64_t)key_lens[b], (int64_t)max_blocks * kBlockSize);
-    f32x4 o[MT];
-    float m_run = decode_wave::kNoMax, l_run = 0.f;
-    if (n > 0)
-        decode_wave::chunk<D, 3, true>(q + qrow * D + 8 * q4, col, pool_k, pool_v, num_blocks, Hkv, g,
-                                       block_tables + (int64_t)b * max_blocks, (n - 1) >> 4, 0, n, scale_log2, o, m_run,
-                                       l_run);
-    else
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) o[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float l = l_run + __shfl_xor(l_run, 16);
-    l += __shfl_xor(l, 32);
-    if (!col) return;
-    const float inv = n > 0 ? 1.f / l : 0.f;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const bf16x4 v = __builtin_convertvector(o[mt] * inv, bf16x4);
-        *reinterpret_cast<u32x2 *>(out + qrow * D + 16 * mt + 4 * q4) = __builtin_bit_cast(u32x2, v);
-    }
+    const int b = blockIdx.x;
+    if (key_lens[b] > 0) return;
+    const int64_t v0 = max(cu_q[b], 0) * row_vecs, v1 = min(cu_q[b + 1], T) * row_vecs;
+    for (int64_t v = v0 + (int64_t)blockIdx.y * kZeroThreads + threadIdx.x; v < v1; v += (int64_t)gridDim.y * kZeroThreads)
+        out[v] = u32x4{0u, 0u, 0u, 0u};
+}
+
+pcr_status check_workspace(int64_t need, const void *workspace, int64_t bytes, const char *who)
+{
+    if (need == 0) return PCR_OK;
+    if (!workspace || bytes < need)
+        return fail(PCR_ERR_INVALID_ARG, "%s: this batch needs a workspace of %lld bytes (%lld given)", who,
+                    (long long)need, (long long)(workspace ? bytes : 0));
+    if ((uintptr_t)workspace & 15) return fail(PCR_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+    return PCR_OK;
 }
 
 pcr_status check_heads(int32_t num_q_heads, int32_t num_kv_heads, const char *who)
@@ -85,6 +69,14 @@ pcr_status pcr_cross_attn_workspace_size(int32_t B, int32_t total_rows, int32_t 
     if (st) return st;
     if (B < 0 || total_rows < 0 || max_keys < 0)
         return fail(PCR_ERR_INVALID_ARG, "%s: negative B, total_rows or max_keys", who);
+    if (B == 0 || total_rows == 0 || max_keys == 0) return PCR_OK;
+    int32_t n_cu = 0;
+    st = device_cu_count(&n_cu, who);
+    if (st) return st;
+    const int64_t rows = (int64_t)total_rows * (num_q_heads / num_kv_heads);
+    const int32_t cols = (int32_t)std::min<int64_t>(rows, decode_max_cols());
+    *bytes = decode_workspace_any(std::min(B, total_rows), num_kv_heads, cols, head_dim, max_keys, n_cu);
+    if (rows > decode_max_cols()) *bytes = std::max(*bytes, cross_tiles_workspace_bytes());
     return PCR_OK;
 }
 
@@ -95,8 +87,6 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
 {
     clear_error();
     const char *who = "pcr_cross_attn";
-    (void)workspace;
-    (void)workspace_bytes;
     pcr_status st = check_pool(pool, who);
     if (st) return st;
     if (B < 0) return fail(PCR_ERR_INVALID_ARG, "%s: B < 0", who);
@@ -107,15 +97,21 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
     if (!(sm_scale > 0.f) || !(sm_scale < 1e30f)) return fail(PCR_ERR_INVALID_ARG, "%s: bad sm_scale", who);
     if (host_cu_q[0] != 0) return fail(PCR_ERR_INVALID_ARG, "%s: cu_q[0] must be 0", who);
     const int D = pool->head_dim, G = num_q_heads / pool->num_kv_heads;
-    int64_t most = 0;
+    if ((int64_t)B * pool->num_kv_heads > (int64_t)1 << 22)
+        return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
+    int64_t most = 0;                       // packed rows of a sequence, at most
+    int64_t most_zero = 0;                  // tokens of one without keys, at most
+    int32_t max_keys = 0;
     for (int32_t b = 0; b < B; ++b) {
         const int64_t s = (int64_t)host_cu_q[b + 1] - host_cu_q[b];
         if (s < 0 || host_key_lens[b] < 0)
             return fail(PCR_ERR_INVALID_ARG, "%s: sequence %d has a negative length", who, b);
-        if (s > 0 && ((int64_t)host_key_lens[b] + kBlockSize - 1) / kBlockSize > max_blocks)
+        if (((int64_t)host_key_lens[b] + kBlockSize - 1) / kBlockSize > max_blocks)
             return fail(PCR_ERR_INVALID_ARG, "%s: sequence %d needs more blocks than max_blocks %d", who, b,
                         max_blocks);
-        most = s > most ? s : most;
+        most = std::max(most, s * G);
+        if (host_key_lens[b] == 0) most_zero = std::max(most_zero, s);
+        max_keys = std::max(max_keys, host_key_lens[b]);
     }
     const int64_t T = host_cu_q[B];
     if (T == 0) return PCR_OK;
@@ -126,17 +122,41 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
         return fail(PCR_ERR_INVALID_ARG, "%s: q/out must be 16-byte aligned", who);
     const uintptr_t qa = (uintptr_t)q, oa = (uintptr_t)out, bytes = (uintptr_t)T * num_q_heads * D * 2;
     if (qa < oa + bytes && oa < qa + bytes) return fail(PCR_ERR_INVALID_ARG, "%s: q and out overlap", who);
-    if (B > 65535 || pool->num_kv_heads > 65535) return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
-    const dim3 grid((unsigned)((most * G + kCols - 1) / kCols), pool->num_kv_heads, B);
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(64), 0, static_cast<hipStream_t>(stream), static_cast<const u16 *>(q),
-                           static_cast<const u16 *>(pool->k), static_cast<const u16 *>(pool->v), pool->num_blocks,
-                           pool->num_kv_heads, block_tables, max_blocks, key_lens, cu_q, (int32_t)T, num_q_heads,
-                           sm_scale * kLog2e, static_cast<u16 *>(out));
-    };
-    if (D == 128) launch(cross_kernel<128>);
-    else launch(cross_kernel<64>);
-    const hipError_t e = hipGetLastError();
+    int32_t n_cu = 0;
+    st = device_cu_count(&n_cu, who);
+    if (st) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    if (most <= decode_max_cols()) {
+        const int32_t cols = (int32_t)most;
+        const int64_t limit = workspace ? std::min<int64_t>(workspace_bytes, kDecodeScratchBytes) : 0;
+        const DecodePlan plan = decode_plan(B, pool->num_kv_heads * cols, pool->num_kv_heads, D, std::max(max_keys, 1),
+                                            n_cu, host_key_lens, limit);
+        st = check_workspace(plan.workspace_bytes, workspace, workspace_bytes, who);
+        if (st) return st;
+        e = launch_cross_rows(q, *pool, block_tables, max_blocks, key_lens, cu_q, B, num_q_heads, (int32_t)T, cols, plan,
+                              sm_scale, out, workspace, s);
+    } else {
+        int64_t tiles = 0;
+        for (int32_t b = 0; b < B; ++b)
+            tiles += ((int64_t)(host_cu_q[b + 1] - host_cu_q[b]) * G + attn_rows_per_workgroup(D) - 1) /
+                     attn_rows_per_workgroup(D);
+        if (tiles * pool->num_kv_heads > (int64_t)1 << 22)
+            return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
+        st = check_workspace(cross_tiles_workspace_bytes(), workspace, workspace_bytes, who);
+        if (st) return st;
+        if (most_zero > 0) {
+            const int64_t row_vecs = (int64_t)num_q_heads * D / 8;
+            const int64_t slices = (most_zero * row_vecs * 16 + kZeroSlice - 1) / kZeroSlice;
+            hipLaunchKernelGGL(cross_zero_kernel, dim3((unsigned)B, (unsigned)std::min<int64_t>(slices, 256)),
+                               dim3(kZeroThreads), 0, s, key_lens, cu_q, (int32_t)T, row_vecs,
+                               static_cast<u32x4 *>(out));
+            e = hipGetLastError();
+            if (e != hipSuccess) return hip_fail(e, "pcr_cross_attn: launch");
+        }
+        e = launch_cross_tiles(q, *pool, block_tables, max_blocks, host_key_lens, host_cu_q, B, num_q_heads, (int32_t)T,
+                               sm_scale, out, workspace, s, n_cu);
+    }
     if (e != hipSuccess) return hip_fail(e, "pcr_cross_attn: launch");
     return PCR_OK;
 }

@@ -52,6 +52,13 @@ hipError_t launch_prefix_prefill_attn(const void *q, const pcr_kv_pool &pool,
                                       const int32_t *host_prefix_lens, const int32_t *host_cu_suffix,
                                       int32_t B, int32_t num_q_heads, int32_t T, float sm_scale, void *out,
                                       hipStream_t s, int auto_schedule, int n_cu);
+// Cross attention by row tiles (attn.hip): every row of a sequence sees its host_key_lens[b] keys;
+// rows of sequences without keys are left.
+// workspace: cross_tiles_workspace_bytes() for a key split, or NULL for none.
+int64_t cross_tiles_workspace_bytes();
+hipError_t launch_cross_tiles(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
+                              const int32_t *host_key_lens, const int32_t *host_cu_q, int32_t B, int32_t num_q_heads,
+                              int32_t T, float sm_scale, void *out, void *workspace, hipStream_t s, int n_cu);
 // Compute units of the current device (queried once per device).
 pcr_status device_cu_count(int32_t *n_cu, const char *who);
 
@@ -81,6 +88,16 @@ int decode_max_cols();
 hipError_t launch_decode_attn(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables,
                               int32_t max_blocks, const int32_t *context_lens, int32_t B, int32_t num_q_heads,
                               const DecodePlan &plan, float sm_scale, void *out, void *workspace, hipStream_t s);
+// Cross attention of sequences with up to `cols` (at most decode_max_cols) packed query rows each:
+// decode_plan of max context >= 1, with num_kv_heads * cols query heads, plans it.
+hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
+                             const int32_t *key_lens, const int32_t *cu_q, int32_t B, int32_t num_q_heads, int32_t T,
+                             int32_t cols, const DecodePlan &plan, float sm_scale, void *out, void *workspace,
+                             hipStream_t s);
+// Bytes that hold every plan decode_plan makes of at most B sequences, whole contexts up to
+// max_context and that many columns.
+int64_t decode_workspace_any(int64_t B, int32_t num_kv_heads, int32_t cols, int32_t head_dim, int32_t max_context,
+                             int32_t n_cu);
 // Size of the allocation-free decode entry point's per-device scratch (decode.hip),
 // and its device address on the current device (taken with hipGetSymbolAddress on the
 // first call per device, then reused).
