@@ -533,8 +533,8 @@ pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, 
  *                    workspace serves every call ordered on one stream; calls that may
  *                    overlap (captured graphs that may run together among them) need their own.
  * Numerics as for pcr_prefix_prefill_attn; slots past n_b are never read into the result.
- * The split of the work follows from the host lengths and the workspace size alone, so
- * repeated calls give identical bits.
+ * The split of the work follows from the host lengths alone, so repeated calls give
+ * identical bits.
  * Errors: as pcr_prefix_prefill_attn, and PCR_ERR_INVALID_ARG when q and out overlap or the
  * workspace is missing, misaligned or too small (the message names the size needed).
  */

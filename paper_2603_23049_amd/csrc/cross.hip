@@ -4,11 +4,11 @@
 //
 // The s * G query rows of one (sequence, kv head) see the same keys, so they are packed
 // (row r = token r / G, head-in-group r % G). A batch whose sequences have up to 16 packed rows
-// each (decode steps, beams) is bound by reading K and V: it runs on the decode kernels
-// (decode.hip), whose waves hold the packed rows as the columns of one matrix tile and cut the
-// keys among them. Any other runs on the row tiles of the prefill kernel (attn.hip) without
-// their causal bound; its sequences of few rows take a decode workgroup in the same launch,
-// those without keys a kernel that writes their zeros.
+// each (decode steps, beams) is bound by reading K and V: its waves hold the packed rows as the
+// columns of one matrix tile and share out the keys of all sequences (cross_rows.hip). Any other
+// runs on the row tiles of the prefill kernel (attn.hip) without their causal bound; its
+// sequences of few rows take a decode workgroup in the same launch. Rows of sequences without
+// keys are zeros that a kernel of their own writes.
 #include <algorithm>
 
 #include "pcr_internal.h"
@@ -18,7 +18,7 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-// Zero rows of the sequences without keys, beside a launch of row tiles. Grid (B, slices).
+// Zero rows of the sequences without keys. Grid (B, slices).
 constexpr int kZeroThreads = 256;
 constexpr int64_t kZeroSlice = 64 << 10;    // bytes of the longest such sequence per workgroup
 __global__ __launch_bounds__(kZeroThreads) void cross_zero_kernel(const int32_t *__restrict__ key_lens,
@@ -31,6 +31,9 @@ __global__ __launch_bounds__(kZeroThreads) void cross_zero_kernel(const int32_t 
     for (int64_t v = v0 + (int64_t)blockIdx.y * kZeroThreads + threadIdx.x; v < v1; v += (int64_t)gridDim.y * kZeroThreads)
         out[v] = u32x4{0u, 0u, 0u, 0u};
 }
+
+// 32-key steps of n keys (decode_wave.h).
+int64_t key_steps(int32_t n) { return ((int64_t)n + 31) / 32; }
 
 pcr_status check_workspace(int64_t need, const void *workspace, int64_t bytes, const char *who)
 {
@@ -75,7 +78,8 @@ pcr_status pcr_cross_attn_workspace_size(int32_t B, int32_t total_rows, int32_t 
     if (st) return st;
     const int64_t rows = (int64_t)total_rows * (num_q_heads / num_kv_heads);
     const int32_t cols = (int32_t)std::min<int64_t>(rows, decode_max_cols());
-    *bytes = decode_workspace_any(std::min(B, total_rows), num_kv_heads, cols, head_dim, max_keys, n_cu);
+    const int64_t steps = std::min(B, total_rows) * (int64_t)num_kv_heads * key_steps(max_keys);
+    *bytes = cross_rows_workspace_bytes(std::min(steps, cross_rows_max_slots(head_dim, n_cu)), cols, head_dim);
     if (rows > decode_max_cols()) *bytes = std::max(*bytes, cross_tiles_workspace_bytes());
     return PCR_OK;
 }
@@ -101,7 +105,8 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
         return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
     int64_t most = 0;                       // packed rows of a sequence, at most
     int64_t most_zero = 0;                  // tokens of one without keys, at most
-    int32_t max_keys = 0;
+    int64_t steps = 0;                      // 32-key steps of all (sequence, kv head) pairs with rows
+    int64_t longest = 0;                    // of one of them, at most
     for (int32_t b = 0; b < B; ++b) {
         const int64_t s = (int64_t)host_cu_q[b + 1] - host_cu_q[b];
         if (s < 0 || host_key_lens[b] < 0)
@@ -111,7 +116,10 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
                         max_blocks);
         most = std::max(most, s * G);
         if (host_key_lens[b] == 0) most_zero = std::max(most_zero, s);
-        max_keys = std::max(max_keys, host_key_lens[b]);
+        if (s > 0) {
+            steps += key_steps(host_key_lens[b]) * pool->num_kv_heads;
+            longest = std::max(longest, key_steps(host_key_lens[b]));
+        }
     }
     const int64_t T = host_cu_q[B];
     if (T == 0) return PCR_OK;
@@ -125,17 +133,21 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
     int32_t n_cu = 0;
     st = device_cu_count(&n_cu, who);
     if (st) return st;
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e;
-    if (most <= decode_max_cols()) {
-        const int32_t cols = (int32_t)most;
-        const int64_t limit = workspace ? std::min<int64_t>(workspace_bytes, kDecodeScratchBytes) : 0;
-        const DecodePlan plan = decode_plan(B, pool->num_kv_heads * cols, pool->num_kv_heads, D, std::max(max_keys, 1),
-                                            n_cu, host_key_lens, limit);
-        st = check_workspace(plan.workspace_bytes, workspace, workspace_bytes, who);
-        if (st) return st;
-        e = launch_cross_rows(q, *pool, block_tables, max_blocks, key_lens, cu_q, B, num_q_heads, (int32_t)T, cols, plan,
-                              sm_scale, out, workspace, s);
+    const bool few = most <= decode_max_cols();
+    CrossRowsPlan plan{};
+    bool cut = false;                       // some (sequence, kv head) lies in two runs
+    if (few) {
+        if (steps > INT32_MAX) return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
+        plan = cross_rows_plan(steps, (int64_t)B * pool->num_kv_heads, longest, D, n_cu);
+        cut = plan.parts > 1;
+        int64_t x = 0;
+        for (int32_t b = 0; b < B && !cut && !plan.parts; ++b) {
+            const int64_t n = host_cu_q[b + 1] > host_cu_q[b] ? key_steps(host_key_lens[b]) : 0;
+            for (int32_t g = 0; n > 0 && g < pool->num_kv_heads && !cut; ++g, x += n)
+                cut = cross_rows_run(plan, steps, x) != cross_rows_run(plan, steps, x + n - 1);
+        }
+        st = check_workspace(cut ? cross_rows_workspace_bytes(plan.slots, (int32_t)most, D) : 0, workspace,
+                             workspace_bytes, who);
     } else {
         int64_t tiles = 0;
         for (int32_t b = 0; b < B; ++b)
@@ -144,19 +156,22 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
         if (tiles * pool->num_kv_heads > (int64_t)1 << 22)
             return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
         st = check_workspace(cross_tiles_workspace_bytes(), workspace, workspace_bytes, who);
-        if (st) return st;
-        if (most_zero > 0) {
-            const int64_t row_vecs = (int64_t)num_q_heads * D / 8;
-            const int64_t slices = (most_zero * row_vecs * 16 + kZeroSlice - 1) / kZeroSlice;
-            hipLaunchKernelGGL(cross_zero_kernel, dim3((unsigned)B, (unsigned)std::min<int64_t>(slices, 256)),
-                               dim3(kZeroThreads), 0, s, key_lens, cu_q, (int32_t)T, row_vecs,
-                               static_cast<u32x4 *>(out));
-            e = hipGetLastError();
-            if (e != hipSuccess) return hip_fail(e, "pcr_cross_attn: launch");
-        }
-        e = launch_cross_tiles(q, *pool, block_tables, max_blocks, host_key_lens, host_cu_q, B, num_q_heads, (int32_t)T,
-                               sm_scale, out, workspace, s, n_cu);
     }
+    if (st) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = hipSuccess;
+    if (most_zero > 0) {
+        const int64_t row_vecs = (int64_t)num_q_heads * D / 8;
+        const int64_t slices = (most_zero * row_vecs * 16 + kZeroSlice - 1) / kZeroSlice;
+        hipLaunchKernelGGL(cross_zero_kernel, dim3((unsigned)B, (unsigned)std::min<int64_t>(slices, 256)),
+                           dim3(kZeroThreads), 0, s, key_lens, cu_q, (int32_t)T, row_vecs, static_cast<u32x4 *>(out));
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && steps > 0)
+        e = few ? launch_cross_rows(q, *pool, block_tables, max_blocks, key_lens, cu_q, B, num_q_heads, (int32_t)T,
+                                    (int32_t)most, steps, plan, cut, sm_scale, out, workspace, s)
+                : launch_cross_tiles(q, *pool, block_tables, max_blocks, host_key_lens, host_cu_q, B, num_q_heads,
+                                     (int32_t)T, sm_scale, out, workspace, s, n_cu);
     if (e != hipSuccess) return hip_fail(e, "pcr_cross_attn: launch");
     return PCR_OK;
 }

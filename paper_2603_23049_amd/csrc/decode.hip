@@ -26,10 +26,6 @@
 // LDS (running max and sum in the log2 domain). With more chunks, each wave
 // writes its unnormalised O, max and sum to the workspace and
 // decode_combine_kernel merges the chunks of each (sequence, head).
-//
-// Cross attention of few rows (CROSS; cross.hip) is the same reading of K/V with other
-// columns: the packed rows (row r = token r / G, head-in-group r % G) of a sequence's tokens,
-// up to 16 together, which all see the sequence's n_b keys. There n_b may be 0 (zero rows).
 #include <algorithm>
 #include <mutex>
 #include <type_traits>
@@ -73,15 +69,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 // otherwise each wave takes a chunk (all n_split of one sequence when those merge in LDS).
 // A template parameter, since telling the two apart in the kernel cost every chunk 0.3 us
 // (12 contexts of 1k-8k); part_keys comes from the host, so that no wave divides for it.
-// CROSS: tokens cu_q[b] .. of sequence b, at most `cols` packed rows each (the decode step: one
-// token, cols = G).
-template <int D, bool K_CACHED, bool SHARED, bool CROSS>
+template <int D, bool K_CACHED, bool SHARED>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) void decode_split_kernel(
     const u16 *__restrict__ q, const u16 *__restrict__ pool_k, const u16 *__restrict__ pool_v,
     int32_t num_blocks, int32_t Hkv, const int32_t *__restrict__ block_tables, int32_t max_blocks,
     const int32_t *__restrict__ context_lens, int32_t B, int32_t Hq, int32_t n_split, int32_t chunk,
     float scale_log2, int32_t lds_merge, int32_t part_keys, u16 *__restrict__ out, float *__restrict__ ws_o,
-    float *__restrict__ ws_ml, const int32_t *__restrict__ cu_q, int32_t T, int32_t cols)
+    float *__restrict__ ws_ml)
 {
     constexpr int MT = D / 16;    // V products (16 dims each)
     const int lane = (int)(threadIdx.x & 63);
@@ -94,27 +88,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) v
     const int g = bg % Hkv, b = bg / Hkv;
     const int n_keys = context_lens[b];
     const int c0 = sp * chunk, c1 = min(n_keys, c0 + chunk);   // the chunk's keys
-    // (a wave of a sequence that merges in LDS stays for the barrier, and where a sequence may
-    // have no key, the one of its first chunk writes zeros)
-    if (c0 >= n_keys && !lds_merge && !(CROSS && sp == 0)) return;
+    if (c0 >= n_keys && !lds_merge) return;        // (a wave of a sequence that merges in LDS stays for the barrier)
     const int kbeg = c0 + (SHARED ? wave * part_keys : 0);
     const int kend = SHARED ? min(c1, kbeg + part_keys) : c1;
     const bool active = kbeg < c1;                 // wave-uniform
     const int last_blk = max(0, min((n_keys - 1) >> 4, max_blocks - 1));   // last block with a visible key
     const int G = Hq / Hkv;
     const int c = lane & 15, q4 = lane >> 4;
-    const int t0 = CROSS ? cu_q[b] : b;
-    const int n_rows = CROSS ? (t0 < 0 ? 0 : min((min(cu_q[b + 1], T) - t0) * G, cols)) : G;
-    const bool col = c < n_rows;
-    if constexpr (CROSS) {
-        if (n_rows <= 0) return;                   // no tokens (the whole workgroup)
-    }
-    const int64_t row = CROSS ? (int64_t)(t0 + c / G) * Hq + g * G + c % G : (int64_t)b * Hq + g * G + c;
+    const bool col = c < G;
+    const int h = g * G + c;
 
     f32x4 o[MT];
     float m_run = decode_wave::kNoMax, l_run = 0.f;
     if (active) {
-        const u16 *qrow = q + (col ? row : (int64_t)t0 * Hq + g * G) * D + 8 * q4;
+        const u16 *qrow = q + ((int64_t)b * Hq + (col ? h : g * G)) * D + 8 * q4;
         decode_wave::chunk<D, 3, K_CACHED>(qrow, col, pool_k, pool_v, num_blocks, Hkv, g, block_tables + (int64_t)b * max_blocks,
                                  last_blk, kbeg, kend, scale_log2, o, m_run, l_run);
     } else {
@@ -154,9 +141,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) v
         }
     }
     if (!col) return;
-    if (lds_merge || (c0 == 0 && c1 >= n_keys)) {   // merged, or the only chunk of its sequence
-        const float inv = CROSS && n_keys <= 0 ? 0.f : 1.f / l_tot;
-        u16 *orow = out + row * D + 4 * q4;
+    if (lds_merge || (c0 == 0 && c1 == n_keys)) {   // merged, or the only chunk of its sequence
+        const float inv = 1.f / l_tot;
+        u16 *orow = out + ((int64_t)b * Hq + h) * D + 4 * q4;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const bf16x4 v = __builtin_convertvector(o[mt] * inv, bf16x4);
@@ -164,7 +151,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) v
         }
         return;
     }
-    const int64_t part = task * (CROSS ? cols : G) + c;
+    const int64_t part = task * G + c;
     float *po = ws_o + part * D + 4 * q4;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4 *>(po + 16 * mt) = o[mt];
@@ -173,29 +160,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1))) v
 
 // One wave per (sequence, query head) of a sequence cut into more than one chunk:
 // out = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c with M = max_c m_c.
-template <int D, bool CROSS>
+template <int D>
 __global__ __launch_bounds__(kThreads) void decode_combine_kernel(
     const float *__restrict__ ws_o, const float *__restrict__ ws_ml, const int32_t *__restrict__ context_lens,
-    int32_t B, int32_t Hkv, int32_t Hq, int32_t n_split, int32_t chunk, u16 *__restrict__ out,
-    const int32_t *__restrict__ cu_q, int32_t T, int32_t cols)
+    int32_t B, int32_t Hkv, int32_t Hq, int32_t n_split, int32_t chunk, u16 *__restrict__ out)
 {
     constexpr int E = D / 64;     // output elements per lane
     const int lane = (int)(threadIdx.x & 63);
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t pair = (int64_t)blockIdx.x * kWaves + wave;
-    const int G = Hq / Hkv;
-    const int C = CROSS ? cols : G;                 // columns of a (sequence, kv head)
-    if (pair >= (int64_t)B * Hkv * C) return;
-    const int b = (int)(pair / (Hkv * C)), gc = (int)(pair % (Hkv * C)), g = gc / C, c = gc % C;
-    const int t0 = CROSS ? cu_q[b] : b;
-    if constexpr (CROSS) {
-        if (t0 < 0 || c >= (min(cu_q[b + 1], T) - t0) * G) return;
-    }
-    const int64_t row = CROSS ? (int64_t)(t0 + c / G) * Hq + g * G + c % G : (int64_t)b * Hq + gc;
+    if (pair >= (int64_t)B * Hq) return;
+    const int h = (int)(pair % Hq), b = (int)(pair / Hq);
+    const int G = Hq / Hkv, g = h / G, c = h % G;
     const int n_keys = context_lens[b];
     const int ns = min((n_keys + chunk - 1) / chunk, n_split);
     if (ns <= 1) return;                            // written by the split kernel
-    const int64_t part0 = ((int64_t)b * Hkv + g) * n_split * C + c;
+    const int64_t part0 = ((int64_t)b * Hkv + g) * n_split * G + c;
     // Up to 64 chunks per pass: lane j reads chunk k0 + j's max and sum (all loads in
     // flight together), the wave reduces them, and the O rows are read eight chunks at a
     // time with their loads issued before any is used. Across passes the running max,
@@ -206,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void decode_combine_kernel(
     for (int k0 = 0; k0 < ns; k0 += 64) {
         const int nk = min(64, ns - k0);
         f32x2 ml = f32x2{-INFINITY, 0.f};
-        if (lane < nk) ml = *reinterpret_cast<const f32x2 *>(ws_ml + 2 * (part0 + (int64_t)(k0 + lane) * C));
+        if (lane < nk) ml = *reinterpret_cast<const f32x2 *>(ws_ml + 2 * (part0 + (int64_t)(k0 + lane) * G));
         float mb = ml[0];
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) mb = fmaxf(mb, __shfl_xor(mb, off));
@@ -225,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void decode_combine_kernel(
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int j = min(j0 + i, nk - 1);       // a chunk past nk is reread, weight 0
-                const float *src = ws_o + (part0 + (int64_t)(k0 + j) * C) * D + E * lane;
+                const float *src = ws_o + (part0 + (int64_t)(k0 + j) * G) * D + E * lane;
 #pragma unroll
                 for (int e = 0; e < E; ++e) po[i][e] = src[e];
             }
@@ -240,7 +220,7 @@ __global__ __launch_bounds__(kThreads) void decode_combine_kernel(
         }
     }
     const float inv = 1.f / L;
-    u16 *orow = out + row * D + E * lane;
+    u16 *orow = out + ((int64_t)b * Hq + h) * D + E * lane;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const __bf16 v = (__bf16)(acc[e] * inv);
@@ -366,29 +346,13 @@ DecodePlan decode_plan(int32_t B, int32_t num_q_heads, int32_t num_kv_heads, int
     return p;
 }
 
-int64_t decode_workspace_any(int64_t B, int32_t num_kv_heads, int32_t cols, int32_t head_dim, int32_t max_context,
-                             int32_t n_cu)
-{
-    // The rule by the largest context takes at most a quarter more chunks than there are waves
-    // (it merges through memory only with more than four chunks a sequence), the one by all
-    // keys what fits the allocation-free scratch; neither more than kMinChunk cuts.
-    const int64_t part_bytes = (int64_t)cols * (head_dim + 2) * 4;
-    const int64_t waves = (int64_t)n_cu * waves_per_cu(head_dim);
-    const int64_t chunks = B * num_kv_heads * (((int64_t)max_context + kMinChunk - 1) / kMinChunk);
-    return std::min(chunks * part_bytes, std::max<int64_t>((waves + waves / 4) * part_bytes, kDecodeScratchBytes));
-}
-
 int decode_max_cols() { return kMaxCols; }
 
-namespace {
-// cols: columns of a (sequence, kv head); cu_q and T: of cross attention.
-template <bool CROSS>
-hipError_t launch_split(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
-                        const int32_t *context_lens, int32_t B, int32_t num_q_heads, const DecodePlan &plan,
-                        float sm_scale, void *out, void *workspace, const int32_t *cu_q, int32_t T, int32_t cols,
-                        hipStream_t s)
+hipError_t launch_decode_attn(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables,
+                              int32_t max_blocks, const int32_t *context_lens, int32_t B, int32_t num_q_heads,
+                              const DecodePlan &plan, float sm_scale, void *out, void *workspace, hipStream_t s)
 {
-    const int Hkv = pool.num_kv_heads, D = pool.head_dim;
+    const int Hkv = pool.num_kv_heads, G = num_q_heads / Hkv, D = pool.head_dim;
     const int64_t n_tasks = (int64_t)B * Hkv * plan.n_split;
     // Up to kWaves chunks of a sequence share one workgroup and merge in LDS when every
     // sequence has all n_split of them; otherwise they go through the workspace and
@@ -402,7 +366,7 @@ hipError_t launch_split(const void *q, const pcr_kv_pool &pool, const int32_t *b
     const dim3 grid((unsigned)(sub > 1 ? n_tasks : (n_tasks + wg_waves - 1) / wg_waves));
     const size_t lds = lds_merge || sub > 1 ? (size_t)wg_waves * 64 * ((D / 16) * 16 + 8) : 0;
     float *ws_o = through_ws ? static_cast<float *>(workspace) : nullptr;
-    float *ws_ml = through_ws ? ws_o + n_tasks * cols * D : nullptr;
+    float *ws_ml = through_ws ? ws_o + n_tasks * G * D : nullptr;
     const float scale_log2 = sm_scale * kLog2e;
     auto *qq = static_cast<const u16 *>(q);
     auto *pk = static_cast<const u16 *>(pool.k);
@@ -411,45 +375,27 @@ hipError_t launch_split(const void *q, const pcr_kv_pool &pool, const int32_t *b
     auto split = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(64 * wg_waves), lds, s, qq, pk, pv, pool.num_blocks, Hkv, block_tables,
                            max_blocks, context_lens, B, num_q_heads, plan.n_split, plan.chunk, scale_log2, lds_merge,
-                           part_keys, oo, ws_o, ws_ml, cu_q, T, cols);
+                           part_keys, oo, ws_o, ws_ml);
     };
     // (a batch that shares chunks leaves SIMDs idle, so it never streams K)
     auto split_d = [&](auto dim) {
         constexpr int DD = decltype(dim)::value;
-        if (sub > 1) split(decode_split_kernel<DD, true, true, CROSS>);
-        else if (plan.k_streamed) split(decode_split_kernel<DD, false, false, CROSS>);
-        else split(decode_split_kernel<DD, true, false, CROSS>);
+        if (sub > 1) split(decode_split_kernel<DD, true, true>);
+        else if (plan.k_streamed) split(decode_split_kernel<DD, false, false>);
+        else split(decode_split_kernel<DD, true, false>);
     };
     if (D == 128) split_d(std::integral_constant<int, 128>{});
     else split_d(std::integral_constant<int, 64>{});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !through_ws) return e;
-    const dim3 cgrid((unsigned)(((int64_t)B * Hkv * cols + kWaves - 1) / kWaves));
-    auto combine = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, cgrid, dim3(kThreads), 0, s, ws_o, ws_ml, context_lens, B, Hkv, num_q_heads,
-                           plan.n_split, plan.chunk, oo, cu_q, T, cols);
-    };
-    if (D == 128) combine(decode_combine_kernel<128, CROSS>);
-    else combine(decode_combine_kernel<64, CROSS>);
+    const dim3 cgrid((unsigned)(((int64_t)B * num_q_heads + kWaves - 1) / kWaves));
+    if (D == 128)
+        hipLaunchKernelGGL(decode_combine_kernel<128>, cgrid, dim3(kThreads), 0, s, ws_o, ws_ml, context_lens, B,
+                           Hkv, num_q_heads, plan.n_split, plan.chunk, oo);
+    else
+        hipLaunchKernelGGL(decode_combine_kernel<64>, cgrid, dim3(kThreads), 0, s, ws_o, ws_ml, context_lens, B,
+                           Hkv, num_q_heads, plan.n_split, plan.chunk, oo);
     return hipGetLastError();
-}
-}  // namespace
-
-hipError_t launch_decode_attn(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables,
-                              int32_t max_blocks, const int32_t *context_lens, int32_t B, int32_t num_q_heads,
-                              const DecodePlan &plan, float sm_scale, void *out, void *workspace, hipStream_t s)
-{
-    return launch_split<false>(q, pool, block_tables, max_blocks, context_lens, B, num_q_heads, plan, sm_scale, out,
-                               workspace, nullptr, B, num_q_heads / pool.num_kv_heads, s);
-}
-
-hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
-                             const int32_t *key_lens, const int32_t *cu_q, int32_t B, int32_t num_q_heads, int32_t T,
-                             int32_t cols, const DecodePlan &plan, float sm_scale, void *out, void *workspace,
-                             hipStream_t s)
-{
-    return launch_split<true>(q, pool, block_tables, max_blocks, key_lens, B, num_q_heads, plan, sm_scale, out,
-                              workspace, cu_q, T, cols, s);
 }
 
 }  // namespace pcr

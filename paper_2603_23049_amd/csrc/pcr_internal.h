@@ -88,16 +88,30 @@ int decode_max_cols();
 hipError_t launch_decode_attn(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables,
                               int32_t max_blocks, const int32_t *context_lens, int32_t B, int32_t num_q_heads,
                               const DecodePlan &plan, float sm_scale, void *out, void *workspace, hipStream_t s);
-// Cross attention of sequences with up to `cols` (at most decode_max_cols) packed query rows each:
-// decode_plan of max context >= 1, with num_kv_heads * cols query heads, plans it.
+// Cross attention of sequences with few packed query rows each (cross_rows.hip): how the 32-key
+// steps of all (sequence, kv head) pairs with rows and keys are cut into `runs` workgroups.
+struct CrossRowsPlan {
+    int32_t runs, waves;   // workgroups, and waves of each
+    int32_t parts;         // runs of a pair, whatever its length; 0: even runs over all steps
+    int32_t slots;         // partial results in the workspace (where some pair is cut)
+};
+// pairs: of all sequences (those without steps too); longest: steps of one pair, at most.
+CrossRowsPlan cross_rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu);
+// Most slots of any plan (none has more than its steps, either).
+int64_t cross_rows_max_slots(int32_t head_dim, int32_t n_cu);
+// The run of an even cut that holds step x.
+inline int64_t cross_rows_run(const CrossRowsPlan &p, int64_t steps, int64_t x)
+{
+    const int64_t base = steps / p.runs, rem = steps % p.runs, big = rem * (base + 1);
+    return x < big ? x / (base + 1) : rem + (x - big) / base;
+}
+int64_t cross_rows_workspace_bytes(int64_t slots, int32_t cols, int32_t head_dim);
+// cols: packed rows of a sequence, at most (up to decode_max_cols); combine: some pair is cut
+// between runs. The rows of sequences without keys are left.
 hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
                              const int32_t *key_lens, const int32_t *cu_q, int32_t B, int32_t num_q_heads, int32_t T,
-                             int32_t cols, const DecodePlan &plan, float sm_scale, void *out, void *workspace,
-                             hipStream_t s);
-// Bytes that hold every plan decode_plan makes of at most B sequences, whole contexts up to
-// max_context and that many columns.
-int64_t decode_workspace_any(int64_t B, int32_t num_kv_heads, int32_t cols, int32_t head_dim, int32_t max_context,
-                             int32_t n_cu);
+                             int32_t cols, int64_t steps, const CrossRowsPlan &plan, bool combine, float sm_scale,
+                             void *out, void *workspace, hipStream_t s);
 // Size of the allocation-free decode entry point's per-device scratch (decode.hip),
 // and its device address on the current device (taken with hipGetSymbolAddress on the
 // first call per device, then reused).
