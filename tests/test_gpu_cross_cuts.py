@@ -22,11 +22,12 @@ def _lens(n, lo, hi, seed, zeros=0):
 @pytest.mark.parametrize("keys,rows,Hq,Hkv,d", [
     (_lens(60, 20, 3000, 1), [1] * 60, 4, 1, 128),                         # even runs, single waves
     (_lens(130, 20, 3000, 2, 20), _lens(130, 0, 2, 3, 30), 2, 1, 128),     # the same, more than 64 sequences, gaps
-    (_lens(40, 100, 4000, 4), [1] * 40, 4, 4, 64),                         # the same, 64 dims
+    (_lens(40, 100, 6000, 4), [1] * 40, 4, 4, 64),                         # the same, 64 dims
     ([13000, 2000, 1000], [1, 1, 1], 8, 8, 128),                           # even runs of four waves
     ([2438, 2438], [1, 2], 14, 2, 128), ([9000], [4], 4, 1, 64),           # parts of a pair
     (_lens(30, 1, 500, 5), [1] * 30, 8, 8, 64), (_lens(9, 1, 90, 6, 2), [2] * 9, 4, 2, 128),   # whole pairs
     (_lens(300, 1, 200, 7, 40), _lens(300, 0, 3, 8, 50), 8, 4, 64), (_lens(300, 30, 60, 9), [1] * 300, 8, 8, 128),
+    (_lens(300, 30, 90, 11), [1] * 300, 2, 1, 128), (_lens(300, 300, 700, 12), [1] * 300, 4, 4, 64),   # two waves; four
     (_lens(70, 1000, 2600, 10), [1] * 70, 16, 1, 128),                     # sixteen columns
 ])
 def test_cuts(keys, rows, Hq, Hkv, d):
