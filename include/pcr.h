@@ -262,8 +262,9 @@ pcr_status pcr_prefix_prefill_attn(const void *q, const pcr_kv_pool *pool,
 
 /*
  * pcr_prefill_attn_set_schedule -- how pcr_prefix_prefill_attn (and the pipelines'
- * attention) divides a launch among workgroups; a tuning and testing control, not
- * part of the method. Every schedule computes the same result (Sec. 2.2).
+ * attention, and pcr_cross_attn with more than 16 packed rows in a sequence) divides a launch
+ * among workgroups; a tuning and testing control, not part of the method. Every schedule
+ * computes the same result (Sec. 2.2).
  *   PCR_ATTN_SCHEDULE_AUTO (the default): row halves from two of their workgroups per
  *     compute unit on, below it key halves, unless the other of the two is estimated to take
  *     4% less time; launches that leave compute units idle take key halves with the keys
@@ -466,8 +467,9 @@ pcr_status pcr_release_blocks(int32_t B, const int32_t *lens, const int32_t *kee
  *   num_axes     1 to 4
  *   scale        finite (1 for a pure rotation)
  * Numerics: the angle is reduced in fp64 (error about |angle| * 2^-52, so positions over
- * the whole int32 range keep their phase), cos and sin are fp32, the products fp32, one
- * rounding to bf16 (nearest even) at the end.
+ * the whole int32 range keep their phase), cos and sin are fp32 (off by at most 2^-22), the
+ * products fp32, one rounding to bf16 (nearest even) at the end; the same bits for a token
+ * whatever else is in the call.
  */
 typedef struct pcr_rope {
     const float *inv_freq;      /* host [rotary_dim / 2], finite */
@@ -535,7 +537,8 @@ pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, 
  * Numerics as for pcr_prefix_prefill_attn; slots past n_b are never read into the result.
  * The split of the work follows from the host lengths alone, so repeated calls give
  * identical bits.
- * Errors: as pcr_prefix_prefill_attn, and PCR_ERR_INVALID_ARG when q and out overlap or the
+ * Errors: as pcr_prefix_prefill_attn, PCR_ERR_UNSUPPORTED beyond 2^30 keys in a sequence or
+ * 2^22 pairs of sequence and kv head, and PCR_ERR_INVALID_ARG when q and out overlap or the
  * workspace is missing, misaligned or too small (the message names the size needed).
  */
 pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t *block_tables, int32_t max_blocks,

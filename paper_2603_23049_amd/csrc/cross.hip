@@ -32,6 +32,8 @@ __global__ __launch_bounds__(kZeroThreads) void cross_zero_kernel(const int32_t 
         out[v] = u32x4{0u, 0u, 0u, 0u};
 }
 
+constexpr int32_t kMaxKeys = 1 << 30;       // positions past a sequence's end still fit int32
+
 // 32-key steps of n keys (decode_wave.h).
 int64_t key_steps(int32_t n) { return ((int64_t)n + 31) / 32; }
 
@@ -114,6 +116,8 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
         if (((int64_t)host_key_lens[b] + kBlockSize - 1) / kBlockSize > max_blocks)
             return fail(PCR_ERR_INVALID_ARG, "%s: sequence %d needs more blocks than max_blocks %d", who, b,
                         max_blocks);
+        if (host_key_lens[b] > kMaxKeys)
+            return fail(PCR_ERR_UNSUPPORTED, "%s: sequence %d has more than 2^30 keys", who, b);
         most = std::max(most, s * G);
         if (host_key_lens[b] == 0) most_zero = std::max(most_zero, s);
         if (s > 0) {

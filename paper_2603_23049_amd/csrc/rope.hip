@@ -102,29 +102,34 @@ __device__ __forceinline__ void turn_unit(const RopeArgs &ra, const int32_t *__r
 __device__ __forceinline__ f32x8 widen(u32x4 v) { return __builtin_convertvector(__builtin_bit_cast(bf16x8, v), f32x8); }
 __device__ __forceinline__ u32x4 narrow(f32x8 v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8)); }
 
+// One pair: the sums written as fused products, so that every kernel (and every size of call)
+// rounds them alike.
+__device__ __forceinline__ void turn_pair(float x, float y, float c, float s, float &r, float &w)
+{
+    r = __builtin_fmaf(x, c, -(y * s));
+    w = __builtin_fmaf(y, c, x * s);
+}
+
 // The unit's two chunks of one head, rotated (fp32 products, rounded once).
 template <bool IL>
 __device__ __forceinline__ void rotate(const Unit &un, u32x4 &a, u32x4 &b)
 {
     const f32x8 x = widen(a), y = widen(b);
-    f32x8 r, w;
+    float r[8], w[8];
     if constexpr (IL) {                                // chunk a holds pairs 0..3, b pairs 4..7
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            r[2 * j] = x[2 * j] * un.c[j] - x[2 * j + 1] * un.s[j];
-            r[2 * j + 1] = x[2 * j + 1] * un.c[j] + x[2 * j] * un.s[j];
-            w[2 * j] = y[2 * j] * un.c[4 + j] - y[2 * j + 1] * un.s[4 + j];
-            w[2 * j + 1] = y[2 * j + 1] * un.c[4 + j] + y[2 * j] * un.s[4 + j];
+            turn_pair(x[2 * j], x[2 * j + 1], un.c[j], un.s[j], r[2 * j], r[2 * j + 1]);
+            turn_pair(y[2 * j], y[2 * j + 1], un.c[4 + j], un.s[4 + j], w[2 * j], w[2 * j + 1]);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            r[j] = x[j] * un.c[j] - y[j] * un.s[j];
-            w[j] = y[j] * un.c[j] + x[j] * un.s[j];
-        }
+        for (int j = 0; j < 8; ++j) turn_pair(x[j], y[j], un.c[j], un.s[j], r[j], w[j]);
     }
-    a = un.turned ? narrow(r) : a;
-    b = un.turned ? narrow(w) : b;
+    const f32x8 rv = {r[0], r[1], r[2], r[3], r[4], r[5], r[6], r[7]};
+    const f32x8 wv = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
+    a = un.turned ? narrow(rv) : a;
+    b = un.turned ? narrow(wv) : b;
 }
 
 // Heads [h0, h1) of the tokens of one workgroup. Threads past the last whole token idle.

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from gpuio import attn_schedule
 from test_gpu_cross import _case, _close, _run
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +56,22 @@ def test_workspace_size_covers_smaller_batches():
         c = _case(keys, rows, 8, 2, 128, 5, poison=False, shared=True)
         q, pk, pv, bt, n, cu = c
         _run(q, pk, pv, bt, n, cu, 2, 128, workspace=torch.empty(big, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("schedule", ["key_halves", "row_halves"])
+@pytest.mark.parametrize("keys,rows,Hq,Hkv,d", [([65, 0, 300], [70, 3, 150], 8, 2, 64), ([129, 1000], [33, 1], 8, 1, 128),
+                                                ([640], [600], 2, 1, 128)])
+def test_row_tile_schedules(schedule, keys, rows, Hq, Hkv, d):
+    c = _case(keys, rows, Hq, Hkv, d, 31)
+    with attn_schedule(schedule):
+        _close(_run(*c, Hkv, d), *c, Hkv, d)
+
+
+@pytest.mark.parametrize("keys,rows,Hq,Hkv,d", [
+    ([6000, 7000], [20, 1], 8, 1, 128), ([5000, 100, 6400, 0], [17, 40, 2, 3], 4, 1, 64),   # keys of row tiles and few rows cut
+    (_lens(140, 1, 100, 13, 9), [20] * 140, 2, 2, 64)])                                # more sequences than one launch's map
+def test_row_tiles(keys, rows, Hq, Hkv, d):
+    c = _case(keys, rows, Hq, Hkv, d, 32)
+    got = _run(*c, Hkv, d)
+    _close(got, *c, Hkv, d)
+    assert torch.equal(got, _run(*c, Hkv, d))

@@ -215,3 +215,30 @@ def test_infinities_and_nan_stay_in_their_pairs():
     bad = ~torch.isfinite(out.cpu().float())
     where = {tuple(i) for i in bad.nonzero().tolist()}
     assert where == {(1, 0, 5), (1, 0, 37), (2, 1, 8), (2, 1, 40)}
+
+
+def test_large_calls_equal_smaller_ones():
+    """Above 128 MiB of input the rows go past the caches; the bits are those of the call in parts."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    T, H, d = 8300, 64, 128                                # 136 MB
+    x = torch.randn(T, H, d, generator=gen, device="cuda").to(torch.bfloat16)
+    pos = torch.randint(0, 10 ** 6, (2, T), generator=gen, device="cuda", dtype=torch.int32)
+    f, axis = _rotation(128, 2)
+    rope = pcr.Rope(f, axis, 2)
+    whole, parts = torch.empty_like(x), torch.empty_like(x)
+    pcr.rope_rows(rope, x, pos, whole)
+    for a, b in ((0, 4000), (4000, 4001), (4001, T)):
+        pcr.rope_rows(rope, x[a:b], pos[:, a:b], parts[a:b])
+    assert torch.equal(whole, parts)
+    Hkv, Hq, nb = 8, 48, T // BS + 2
+    slots = torch.randperm(nb, generator=gen, device="cuda").repeat_interleave(BS)[:T].to(torch.int32) * BS
+    slots += torch.arange(T, device="cuda", dtype=torch.int32) % BS
+    q, k, v = x.flatten(1).split([Hq * d, Hkv * d, Hkv * d], dim=1)
+    pools = [pcr.KVPool(torch.zeros(nb, Hkv, BS * d, dtype=torch.bfloat16, device="cuda"),
+                        torch.zeros(nb, Hkv, BS * d, dtype=torch.bfloat16, device="cuda"), Hkv, d) for _ in range(2)]
+    outs = [torch.empty(T, Hq, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    pcr.rope_append_kv(rope, pools[0], q, k, v, pos, slots, Hq, outs[0])
+    for a, b in ((0, 17), (17, 5000), (5000, T)):
+        pcr.rope_append_kv(rope, pools[1], q[a:b], k[a:b], v[a:b], pos[:, a:b], slots[a:b], Hq, outs[1][a:b])
+    assert torch.equal(outs[0], outs[1]) and torch.equal(pools[0].k, pools[1].k) and torch.equal(pools[0].v, pools[1].v)
+    assert torch.equal(outs[0], whole[:, :Hq])

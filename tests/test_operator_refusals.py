@@ -122,7 +122,8 @@ def test_cross():
                dict(bt=None), dict(cu=(0, 1, 2 ** 31 - 1)), dict(q=A + 2), dict(out=A + 4), dict(out=A + 512),
                dict(pool=None)):
         assert _cross(**kw) == INV, kw
-    for kw in (dict(Hq=3), dict(Hq=0), dict(pool=_pool(d=80)), dict(pool=_pool(bs=32))):
+    for kw in (dict(Hq=3), dict(Hq=0), dict(pool=_pool(d=80)), dict(pool=_pool(bs=32)), dict(n=(5, 2 ** 30 + 1), mb=2 ** 27),
+               dict(B=2 ** 22, pool=_pool(Hkv=2))):
         assert _cross(**kw) == UNS, kw
     assert _cross(B=0) == pcr.PCR_OK and _cross(cu=(0, 0, 0)) == pcr.PCR_OK
 
