@@ -11,8 +11,10 @@
 // hold the up to 16 packed rows of the pair as matrix columns (decode_wave.h) and merge in LDS. A
 // segment that is its whole pair writes the rows; the others leave (O, max, sum) in the
 // workspace, at most two of a run (its first and its last), and cross_rows_combine_kernel
-// merges the parts of each pair. K loads are ordinary ones (past the caches: ragged batches of
-// 64 207 instead of 186 us, equal ones 265 instead of 259, small ones up to 5% less).
+// merges the parts of each pair. K loads go past the caches, except in whole pairs, whose waves
+// end at different times (one token each, 32 / 8 heads of 128, ordinary loads and past the caches:
+// 64 ragged sequences of up to 6404 keys in even runs 187 and 181 us, as whole pairs 186 and 207;
+// one sequence of 6404 keys, in parts, 14.9 and 14.1 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -27,6 +29,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16;
+
+// What a run is (see above).
+enum Cut { kWhole, kParts, kEven };
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStepKeys = decode_wave::kStepKeys;
@@ -98,8 +103,7 @@ __device__ __forceinline__ bool find_sequence(const CrossArgs &a, const int32_t 
     return false;
 }
 
-// PAIRS: a run is a part of one pair; otherwise an even share of all steps.
-template <int D, int WAVES, bool PAIRS>
+template <int D, int WAVES, int CUT>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1))) void cross_rows_kernel(
     const CrossArgs a, const u16 *__restrict__ q, const u16 *__restrict__ pool_k, const u16 *__restrict__ pool_v,
     const int32_t *__restrict__ block_tables, const int32_t *__restrict__ key_lens, const int32_t *__restrict__ cu_q,
@@ -114,7 +118,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
     const int G = a.Hq / a.Hkv, ct = c / G, cg = c - ct * G;
     int x0, x1;
     At at;
-    if constexpr (PAIRS) {                             // part `run % parts` of pair `run / parts`
+    if constexpr (CUT != kEven) {                      // part `run % parts` of pair `run / parts`
         const int pair = run / a.parts, part = run - pair * a.parts;
         at.b = pair / a.Hkv;
         at.st = pair_steps(a, key_lens, cu_q, at.b, at.n_keys, at.t0, at.rows);
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
         if (!find_sequence(a, key_lens, cu_q, x0, at)) return;
     }
     for (int x = x0; x < x1;) {
-        while (!PAIRS && x >= at.first + at.st * a.Hkv) {   // on to the next sequence with steps
+        while (CUT == kEven && x >= at.first + at.st * a.Hkv) {   // on to the next sequence with steps
             at.first += at.st * a.Hkv;
             if (++at.b >= a.B) return;
             at.st = pair_steps(a, key_lens, cu_q, at.b, at.n_keys, at.t0, at.rows);
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
         float m = decode_wave::kNoMax, l = 0.f;
         if (kbeg < kend) {
             const u16 *qrow = q + (col ? row : (int64_t)t0 * a.Hq + g * G) * D + 8 * q4;
-            decode_wave::chunk<D, 3, true>(qrow, col, pool_k, pool_v, a.num_blocks, a.Hkv, g,
+            decode_wave::chunk<D, 3, CUT == kWhole>(qrow, col, pool_k, pool_v, a.num_blocks, a.Hkv, g,
                                                block_tables + (int64_t)b * a.max_blocks, (n_keys - 1) >> 4, kbeg, kend,
                                                a.scale_log2, o, m, l);
         } else {
@@ -191,7 +195,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
                     *reinterpret_cast<u32x2 *>(orow + 16 * mt) = __builtin_bit_cast(u32x2, v);
                 }
             } else {
-                const int64_t part = (int64_t)(PAIRS ? run : 2 * run + (x == x0 ? 0 : 1)) * a.cols + c;
+                const int64_t part = (int64_t)(CUT != kEven ? run : 2 * run + (x == x0 ? 0 : 1)) * a.cols + c;
                 float *po = ws_o + part * D + 4 * q4;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4 *>(po + 16 * mt) = o[mt];
@@ -199,14 +203,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
             }
         }
         x += s1 - s0;
-        if constexpr (WAVES > 1 && !PAIRS) __syncthreads();   // the next segment writes the parts again
+        if constexpr (WAVES > 1 && CUT == kEven) __syncthreads();   // the next segment writes the parts again
     }
 }
 
 // One wave per (pair, column) of a pair cut between runs:
 // out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p with M = max_p m_p, in the parts' order.
 constexpr int kCombineWaves = 4;
-template <int D, bool PAIRS>
+template <int D, int CUT>
 __global__ __launch_bounds__(64 * kCombineWaves) void cross_rows_combine_kernel(
     const CrossArgs a, const int32_t *__restrict__ key_lens, const int32_t *__restrict__ cu_q,
     const float *__restrict__ ws_o, const float *__restrict__ ws_ml, u16 *__restrict__ out)
@@ -222,8 +226,8 @@ __global__ __launch_bounds__(64 * kCombineWaves) void cross_rows_combine_kernel(
     const int st = pair_steps(a, key_lens, cu_q, b, n, t0, rows);
     if (st == 0 || c >= rows) return;
     int slot0, odd = 0, parts;    // slot of the first part (plus odd), slots from part to part, parts
-    constexpr int kStride = PAIRS ? 1 : 2;
-    if constexpr (PAIRS) {
+    constexpr int kStride = CUT == kParts ? 1 : 2;
+    if constexpr (CUT == kParts) {
         const int per = (st + a.parts - 1) / a.parts;
         parts = (st + per - 1) / per;
         slot0 = pc * a.parts;
@@ -372,17 +376,19 @@ hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32
                                static_cast<const u16 *>(q), static_cast<const u16 *>(pool.k),
                                static_cast<const u16 *>(pool.v), block_tables, key_lens, cu_q, oo, ws_o, ws_ml);
         };
-        if (plan.parts) {
-            if constexpr (D == 64) {
-                if (plan.waves == 8) rows(cross_rows_kernel<D, 8, true>);
-            }
-            if (plan.waves == 4) rows(cross_rows_kernel<D, 4, true>);
-            else if (plan.waves == 2) rows(cross_rows_kernel<D, 2, true>);
-            else if (plan.waves == 1) rows(cross_rows_kernel<D, 1, true>);
+        if (plan.parts > 1) {
+            rows(cross_rows_kernel<D, 4, kParts>);
+        } else if (!plan.parts) {
+            if (plan.waves == 4) rows(cross_rows_kernel<D, 4, kEven>);
+            else rows(cross_rows_kernel<D, 1, kEven>);
         } else if (plan.waves == 4) {
-            rows(cross_rows_kernel<D, 4, false>);
-        } else {
-            rows(cross_rows_kernel<D, 1, false>);
+            rows(cross_rows_kernel<D, 4, kWhole>);
+        } else if (plan.waves == 2) {
+            rows(cross_rows_kernel<D, 2, kWhole>);
+        } else if (plan.waves == 1) {
+            rows(cross_rows_kernel<D, 1, kWhole>);
+        } else if constexpr (D == 64) {
+            rows(cross_rows_kernel<D, 8, kWhole>);
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || !combine) return e;
@@ -391,8 +397,8 @@ hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32
             hipLaunchKernelGGL(kernel, dim3((unsigned)((tasks + kCombineWaves - 1) / kCombineWaves)),
                                dim3(64 * kCombineWaves), 0, s, a, key_lens, cu_q, ws_o, ws_ml, oo);
         };
-        if (plan.parts) merge(cross_rows_combine_kernel<D, true>);
-        else merge(cross_rows_combine_kernel<D, false>);
+        if (plan.parts) merge(cross_rows_combine_kernel<D, kParts>);
+        else merge(cross_rows_combine_kernel<D, kEven>);
         return hipGetLastError();
     };
     if (pool.head_dim == 128) return go(std::integral_constant<int, 128>{});
