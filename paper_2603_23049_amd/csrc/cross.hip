@@ -80,7 +80,8 @@ pcr_status pcr_cross_attn_workspace_size(int32_t B, int32_t total_rows, int32_t 
     if (st) return st;
     const int64_t rows = (int64_t)total_rows * (num_q_heads / num_kv_heads);
     const int32_t cols = (int32_t)std::min<int64_t>(rows, decode_max_cols());
-    const int64_t steps = std::min(B, total_rows) * (int64_t)num_kv_heads * key_steps(max_keys);
+    // (sequences without rows count: a plan of parts has slots for them too)
+    const int64_t steps = (int64_t)B * num_kv_heads * key_steps(max_keys);
     *bytes = cross_rows_workspace_bytes(std::min(steps, cross_rows_max_slots(head_dim, n_cu)), cols, head_dim);
     if (rows > decode_max_cols()) *bytes = std::max(*bytes, cross_tiles_workspace_bytes());
     return PCR_OK;

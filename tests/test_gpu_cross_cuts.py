@@ -58,6 +58,12 @@ def test_workspace_size_covers_smaller_batches():
         _run(q, pk, pv, bt, n, cu, 2, 128, workspace=torch.empty(big, dtype=torch.uint8, device="cuda"))
 
 
+def test_workspace_size_with_sequences_without_rows():
+    """Two of 64 sequences have a row: the size for 2 rows in all serves a plan of parts of all 64."""
+    c = _case([800, 800] + [0] * 62, [1, 1] + [0] * 62, 1, 1, 64, 2)
+    _close(_run(*c, 1, 64), *c, 1, 64)
+
+
 @pytest.mark.parametrize("schedule", ["key_halves", "row_halves"])
 @pytest.mark.parametrize("keys,rows,Hq,Hkv,d", [([65, 0, 300], [70, 3, 150], 8, 2, 64), ([129, 1000], [33, 1], 8, 1, 128),
                                                 ([640], [600], 2, 1, 128)])
