@@ -194,7 +194,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
                     const bf16x4 v = __builtin_convertvector(o[mt] * inv, bf16x4);
                     *reinterpret_cast<u32x2 *>(orow + 16 * mt) = __builtin_bit_cast(u32x2, v);
                 }
-            } else {
+            } else if (ws_o) {                         // (device lengths that are not the host's may cut more pairs)
                 const int64_t part = (int64_t)(CUT != kEven ? run : 2 * run + (x == x0 ? 0 : 1)) * a.cols + c;
                 float *po = ws_o + part * D + 4 * q4;
 #pragma unroll
@@ -354,7 +354,8 @@ hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32
                              int32_t cols, int64_t steps, const CrossRowsPlan &plan, bool combine, float sm_scale,
                              void *out, void *workspace, hipStream_t s)
 {
-    auto *ws_o = static_cast<float *>(workspace);
+    // (where no pair is cut nothing is written there: no workspace, whatever its size, reaches the kernel)
+    auto *ws_o = combine ? static_cast<float *>(workspace) : nullptr;
     float *ws_ml = ws_o ? ws_o + (int64_t)plan.slots * cols * pool.head_dim : nullptr;
     auto *oo = static_cast<u16 *>(out);
     CrossArgs a{};
