@@ -494,7 +494,7 @@ typedef struct pcr_rope {
  *   q_out            device bf16 [T][Hq][d] contiguous, 16-byte aligned; may be q itself
  *                    when q_stride is Hq * d, otherwise the two must not overlap
  *   num_q_heads      0: no Q (q and q_out are not read)
- * k_new and v_new must not overlap q_out or the pool. Errors: as pcr_append_kv;
+ * k_new and v_new must not overlap q_out, none of the three the pool. Errors: as pcr_append_kv;
  * PCR_ERR_INVALID_ARG for the stride, alignment, overlap and rope conditions above.
  */
 pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, const void *q, int64_t q_stride,
@@ -508,7 +508,8 @@ pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, con
  * that go to no pool). inverse != 0 applies the transposed map (sin negated): the gradient
  * with respect to x of a gradient with respect to out, and with scale 1 the undoing.
  *   head_dim  a multiple of 16 up to 256 (else PCR_ERR_UNSUPPORTED)
- * out may be x itself when the strides are equal, otherwise they must not overlap; both
+ * out may be x itself when the strides are equal, otherwise they must not overlap (with equal
+ * strides they may be different parts of the same rows); both
  * 16-byte aligned, strides multiples of 8 and at least num_heads * head_dim. T = 0 is a no-op.
  */
 pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, const int32_t *positions,

@@ -340,6 +340,7 @@ __global__ __launch_bounds__(kRowThreads) void rope_append_rows_kernel(const Rop
 // 128: 3.8 us, 4.2 with twice the line).
 constexpr int kHeads = 4;
 constexpr int kMinWgs = 256;
+constexpr int kMaxGridY = 65535;  // more head groups are not launched: they take more heads
 // K/V workgroups wanted; a tile's kv heads are dealt to as many as that takes (2048 to 8192 alike).
 constexpr int kKvWgs = 2048;
 // Bytes of K and Q up to which a call runs as rows (rope_append_rows_kernel). One token of each
@@ -395,11 +396,21 @@ pcr_status check_rows(const void *x, int64_t stride, int64_t width, const char *
     return PCR_OK;
 }
 
+bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
+{
+    return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+// From the first element of T rows to the last.
+int64_t span(int32_t T, int64_t stride, int64_t width) { return ((int64_t)(T - 1) * stride + width) * 2; }
+
 bool rows_overlap(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int32_t T, int64_t width)
 {
-    const uintptr_t a0 = (uintptr_t)a, a1 = a0 + ((uintptr_t)(T - 1) * a_stride + width) * 2;
-    const uintptr_t b0 = (uintptr_t)b, b1 = b0 + ((uintptr_t)(T - 1) * b_stride + width) * 2;
-    return a0 < b1 && b0 < a1;
+    if (!overlap(a, span(T, a_stride, width), b, span(T, b_stride, width))) return false;
+    if (a_stride != b_stride) return true;
+    // Parts of the same rows: the distance within a row says it.
+    const uint64_t row = (uint64_t)a_stride * 2, bytes = (uint64_t)width * 2;
+    const uint64_t d = (a > b ? (uintptr_t)a - (uintptr_t)b : (uintptr_t)b - (uintptr_t)a) % row;
+    return d < bytes || row - d < bytes;
 }
 
 hipError_t launch_rows(const RopeArgs &ra, const void *x, int64_t x_stride, const int32_t *positions,
@@ -408,7 +419,8 @@ hipError_t launch_rows(const RopeArgs &ra, const void *x, int64_t x_stride, cons
 {
     const int per = kThreads / (D / (2 * kUnit));
     const int64_t tiles = ((int64_t)T + per - 1) / per;
-    const int32_t heads = H >= kHeads && tiles * ((H + kHeads - 1) / kHeads) >= kMinWgs ? kHeads : 1;
+    int32_t heads = H >= kHeads && tiles * ((H + kHeads - 1) / kHeads) >= kMinWgs ? kHeads : 1;
+    heads = std::max(heads, (H + kMaxGridY - 1) / kMaxGridY);
     const dim3 grid((unsigned)tiles, (unsigned)((H + heads - 1) / heads));
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, ra, static_cast<const u16 *>(x), x_stride, positions,
@@ -501,6 +513,15 @@ pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, con
         if (!(q == q_out && q_stride == q_width) && rows_overlap(q, q_stride, q_out, q_width, T, q_width))
             return fail(PCR_ERR_INVALID_ARG, "%s: q and q_out overlap (and are not one array)", who);
     }
+    const int64_t k_span = span(T, k_stride, kv_width), v_span = span(T, v_stride, kv_width);
+    const int64_t q_span = num_q_heads > 0 ? T * q_width * 2 : 0;
+    if (overlap(k_new, k_span, q_out, q_span) || overlap(v_new, v_span, q_out, q_span))
+        return fail(PCR_ERR_INVALID_ARG, "%s: q_out overlaps k_new or v_new", who);
+    const int64_t pool_bytes = pool->num_blocks * kv_block_bytes(pool->block_size, pool->num_kv_heads, pool->head_dim);
+    for (const void *x : {pool->k, pool->v})
+        if (overlap(x, pool_bytes, k_new, k_span) || overlap(x, pool_bytes, v_new, v_span) ||
+            overlap(x, pool_bytes, q_out, q_span))
+            return fail(PCR_ERR_INVALID_ARG, "%s: k_new, v_new or q_out overlaps the pool", who);
     AppendArgs aa{};
     aa.pool_k = static_cast<u16 *>(pool->k);
     aa.pool_v = static_cast<u16 *>(pool->v);

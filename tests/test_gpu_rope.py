@@ -87,6 +87,28 @@ def test_rows_strided_scaled_and_one_axis_default():
     assert torch.equal(wd.cpu()[:, same], wide[:, same])
 
 
+def test_rows_into_another_part_of_the_same_rows():
+    gen = _gen(6)
+    T, H, d = 45, 2, 64
+    wide = _bf16(gen, T, 3 * H * d)
+    pos = _positions(gen, 1, T, 5000)
+    f, axis = _rotation(64, 1)
+    wd = wide.cuda()
+    pcr.rope_rows(pcr.Rope(f), wd[:, 256:].unflatten(1, (H, d)), pos.cuda(), wd[:, 128:256].unflatten(1, (H, d)))
+    got = wd.cpu()
+    _close(got[:, 128:256].unflatten(1, (H, d)), wide[:, 256:].unflatten(1, (H, d)), pos, f, axis, 0)
+    assert torch.equal(got[:, :128], wide[:, :128]) and torch.equal(got[:, 256:], wide[:, 256:])
+
+
+def test_more_heads_than_a_grid_has_rows():
+    gen = _gen(7)
+    x, pos = _bf16(gen, 1, 300001, 16), _positions(gen, 1, 1, 5000)
+    f, axis = _rotation(16, 1)
+    out = torch.empty_like(x, device="cuda")
+    pcr.rope_rows(pcr.Rope(f), x.cuda(), pos.cuda(), out)
+    _close(out, x, pos, f, axis, 0)
+
+
 def test_rows_gradient_is_the_transpose():
     """<rope(x), g> = <x, rope_inverse(g)> and, in fp32 rotations of the same kernel's inputs,
     differences along x: the map is linear, so a difference is the map of the difference."""

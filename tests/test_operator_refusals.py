@@ -93,6 +93,10 @@ def test_append_rows():
         if kw == dict(out=A):
             kw = dict(out=A, qs=264)                 # the same array, but not back to back
         assert _append(**kw) == INV, kw
+    inside = A + 8192                                # of the pool's K: 4 blocks of 4 KB
+    for kw in (dict(out=A + 16368), dict(k=inside), dict(v=inside), dict(v=(A << 4) + 16368), dict(out=(A << 4) - 16),
+               dict(out=(A << 1) - 16), dict(k=(A << 8) + 16, ks=1024), dict(v=(A << 8) + 5104)):
+        assert _append(**kw, q=A << 12) == INV and "overlap" in pcr.last_error(), kw
     assert _append(Hq=3) == UNS and _append(T=2 ** 27 + 1, ps=2 ** 28) == UNS
     assert _append(pool=_pool(d=96)) == UNS and _append(pool=_pool(bs=8)) == UNS
     assert pcr.lib().pcr_rope_append_kv(None, _pool(), A, 256, A, 128, A, 128, A, 10, A, 10, 4, A << 8, None) == INV
@@ -102,6 +106,10 @@ def test_plain_rows():
     for kw in (dict(H=0), dict(x=None), dict(out=None), dict(xs=120), dict(os=127), dict(x=A + 2), dict(out=A + 256),
                dict(out=A, os=136)):
         assert _rows(**kw) == INV, kw
+    # parts of the same rows: overlapping by 8 elements at either end, or whole rows apart
+    for kw in (dict(xs=256, os=256, out=A + 240), dict(xs=256, os=256, x=A + 272, out=A), dict(out=A + 512 * 3, xs=256, os=256),
+               dict(out=A + 512 * 3 + 272, xs=256, os=256)):
+        assert _rows(**kw) == INV and "overlap" in pcr.last_error(), kw
     assert _rows(T=2 ** 27 + 1, ps=2 ** 28) == UNS and _rows(H=2 ** 25, xs=2 ** 31, os=2 ** 31) == UNS
     for d in (0, 8, 72, 272, -16):
         assert _rows(d=d) == UNS
