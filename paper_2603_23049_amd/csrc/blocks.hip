@@ -15,6 +15,8 @@
 //
 // Sums saturate at 2^31 - 1 (a saturating sum of non-negative numbers does not depend on
 // the grouping), so no length, however wrong, wraps around into a fit.
+#include <algorithm>
+
 #include "pcr_internal.h"
 
 namespace pcr {
@@ -222,13 +224,20 @@ constexpr int kBigBatch = 256;
 // 4.0 us, 4.7 with two rows a thread, 6.3 with four, 130 with one workgroup; 160 thousand released ids
 // of 500 rows 4.7, 5.4, 6.9 and 134; a decode step of 64 3.0).
 constexpr int kPerThread = 4;
+// Chunks of sequences from which a tile has more than one row per thread: every workgroup scans all
+// chunks, so tiles grow with them, and the work of a call with it instead of with its square
+// (262144 sequences: release of a million ids 2006 -> 537 us, a token each in 1262144 rows
+// 2648 -> 559; 65536 alike; a line of 4 chunks takes up to 16% more).
+constexpr int kManyChunks = 16;
 
 // One launch, or two where the state is updated in place and several workgroups read it.
 template <class Args>
 hipError_t launch_tiles(void (*small)(Args), void (*big)(Args), Args a, int64_t rows, bool in_place, hipStream_t s)
 {
     const int threads = a.B <= kBigBatch ? 256 : 1024;
-    a.tile = in_place && rows <= threads * kPerThread ? threads * kPerThread : threads;
+    const int64_t chunks = ((int64_t)a.B + threads - 1) / threads;
+    a.tile = in_place && rows <= threads * kPerThread ? threads * kPerThread
+                                                      : threads * (int32_t)std::max<int64_t>(1, chunks / kManyChunks);
     const int64_t wgs = rows > a.tile ? (rows + a.tile - 1) / a.tile : 1;
     auto kernel = a.B <= kBigBatch ? small : big;
     a.state = wgs == 1 || !in_place;

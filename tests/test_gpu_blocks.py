@@ -80,6 +80,24 @@ def test_assign_equals_definition(B, p_max, s_max, extra):
     assert np.array_equal(got[1], want[1]) and (got[2] == GUARD).all()
 
 
+def test_many_sequences():
+    """Tiles of several rows per thread (they grow with the sequences), for both directions."""
+    B = 40000
+    rng = np.random.Generator(np.random.PCG64(17))
+    p, s = rng.integers(0, 40, size=B), rng.integers(0, 3, size=B)
+    num_blocks = int(sum(-(-(a + b) // BS) for a, b in zip(p, s))) + 5
+    bt, free = _setup(p, s, num_blocks, 6)
+    table = _check(p, s, bt, free, len(free), num_blocks, int(s.sum()) + 700)[0].reshape(B, -1)
+    lens, keep = p + s, np.where(rng.random(B) < 0.5, p, 0)
+    stack = _i32(np.full(num_blocks, -9))
+    count, status = _i32([3]), _i32([0, 0, 0])
+    pcr.release_blocks(_i32(lens), _i32(keep), _i32(table), stack, count, num_blocks, count, status)
+    want = [table[b, e] for b in range(B) for e in range(-(-keep[b] // BS), -(-lens[b] // BS))]
+    assert status.tolist() == [B, len(want), len(want)] and count.item() == 3 + len(want)
+    got = stack.cpu().numpy()
+    assert np.array_equal(got[3:3 + len(want)], np.array(want[::-1])) and (got[3 + len(want):] == -9).all()
+
+
 def test_assign_at_block_edges():
     p = [0, 15, 16, 17, 31, 32, 0, 16, 0]
     s = [16, 1, 1, 15, 2, 16, 17, 0, 0]
