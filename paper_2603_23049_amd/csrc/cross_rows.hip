@@ -300,10 +300,10 @@ __global__ __launch_bounds__(64 * kCombineWaves) void cross_rows_combine_kernel(
 // all steps at the rate of a full device, a compute unit cu for one step (its own limit, about
 // 40 GB/s), and the constants are what the launches take with nothing to read. Measured, one run a
 // pair / some runs a pair / even runs: one token of 187 sequences of 1064 keys (16 / 2 heads of 128)
-// 44 / 48 / 47, of 2 of 2438 (28 / 4) 31 / 12 / 16, of 53 of 1034-8276 (64 / 8) 219 / 207 / 168 and
-// of 45 of 828-6627 168 / 159 / 129. (The decode entry point's plan, chunks of one size for the
-// whole batch, takes 48, 12, 252 and 184 there. Over the 330 this choice takes 7% less than that
-// plan, 36% at best; the worst, a call of 13 us, 14% more.)
+// 42 / - / 44, of 2 of 2438 (28 / 4) 32 / 12 / 17, of 53 of 1034-8276 (64 / 8) 212 / - / 163 and
+// of 45 of 828-6627 161 / - / 115. (The decode entry point's plan, chunks of one size for the
+// whole batch, takes 48, 12, 252 and 184 there. Over the 330 this choice takes 8% less than that
+// plan, 37% at best; the worst, a call of 14 us, 14% more.)
 CrossRowsPlan cross_rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu)
 {
     CrossRowsPlan p{};
