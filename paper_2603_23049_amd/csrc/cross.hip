@@ -160,7 +160,8 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
                      attn_rows_per_workgroup(D);
         if (tiles * pool->num_kv_heads > (int64_t)1 << 22)
             return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
-        st = check_workspace(cross_tiles_workspace_bytes(), workspace, workspace_bytes, who);
+        // (without keys only zero rows are written)
+        st = check_workspace(steps > 0 ? cross_tiles_workspace_bytes() : 0, workspace, workspace_bytes, who);
     }
     if (st) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
