@@ -495,7 +495,8 @@ typedef struct pcr_rope {
  *                    when q_stride is Hq * d, otherwise the two must not overlap
  *   num_q_heads      0: no Q (q and q_out are not read)
  * k_new and v_new must not overlap q_out, none of the three the pool. Errors: as pcr_append_kv;
- * PCR_ERR_INVALID_ARG for the stride, alignment, overlap and rope conditions above.
+ * PCR_ERR_INVALID_ARG for the stride, alignment, overlap and rope conditions above;
+ * PCR_ERR_UNSUPPORTED beyond 2^27 tokens or 2^32 threads (about one per 16 dims of 4 query heads).
  */
 pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, const void *q, int64_t q_stride,
                               const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,

@@ -31,7 +31,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 128;
 constexpr int kMaxAxes = 4;
-constexpr int32_t kMaxTokens = 1 << 27;   // keeps every grid inside 2^32 threads
+constexpr int32_t kMaxTokens = 1 << 27;   // 2^31 threads at most for plain rows (launch_append checks its own)
 constexpr int kUnit = 8;          // pairs of a unit
 constexpr int kTile = 32;         // new tokens of a K/V workgroup (append_tile.h)
 
@@ -434,7 +434,9 @@ hipError_t launch_rows(const RopeArgs &ra, const void *x, int64_t x_stride, cons
     return hipGetLastError();
 }
 
-hipError_t launch_append(const RopeArgs &ra, AppendArgs aa, int D, hipStream_t s)
+pcr_status launched(hipError_t e) { return e == hipSuccess ? PCR_OK : hip_fail(e, "pcr_rope_append_kv: launch"); }
+
+pcr_status launch_append(const RopeArgs &ra, AppendArgs aa, int D, hipStream_t s)
 {
     if ((int64_t)aa.T * (aa.Hkv + aa.Hq) * D * 2 <= kRowsBytes) {
         const int rows = kRowThreads / (D / (2 * kUnit));
@@ -448,7 +450,7 @@ hipError_t launch_append(const RopeArgs &ra, AppendArgs aa, int D, hipStream_t s
             if (ra.interleaved) go(rope_append_rows_kernel<64, true>);
             else go(rope_append_rows_kernel<64, false>);
         }
-        return hipGetLastError();
+        return launched(hipGetLastError());
     }
     const int per = kThreads / (D / (2 * kUnit));
     const int64_t kv_tiles = ((int64_t)aa.T + kTile - 1) / kTile, q_tiles = ((int64_t)aa.T + per - 1) / per;
@@ -459,7 +461,11 @@ hipError_t launch_append(const RopeArgs &ra, AppendArgs aa, int D, hipStream_t s
     aa.q_heads = kHeads;
     aa.q_groups = (aa.Hq + aa.q_heads - 1) / aa.q_heads;
     const int64_t in_bytes = (int64_t)aa.T * (aa.Hq + 2 * aa.Hkv) * D * 2;
-    const dim3 grid((unsigned)(aa.kv_wgs + q_tiles * aa.q_groups));
+    const int64_t wgs = aa.kv_wgs + q_tiles * aa.q_groups;
+    if (wgs * kThreads > (int64_t)UINT32_MAX)
+        return fail(PCR_ERR_UNSUPPORTED, "pcr_rope_append_kv: %d tokens of %d query heads take 2^32 threads or more",
+                    aa.T, aa.Hq);
+    const dim3 grid((unsigned)wgs);
     auto launch = [&](auto dim) {
         constexpr int DD = decltype(dim)::value;
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, ra, aa); };
@@ -471,7 +477,7 @@ hipError_t launch_append(const RopeArgs &ra, AppendArgs aa, int D, hipStream_t s
     };
     if (D == 128) launch(std::integral_constant<int, 128>{});
     else launch(std::integral_constant<int, 64>{});
-    return hipGetLastError();
+    return launched(hipGetLastError());
 }
 
 }  // namespace
@@ -539,9 +545,7 @@ pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, con
     aa.Hkv = pool->num_kv_heads;
     aa.Hq = num_q_heads;
     aa.T = T;
-    const hipError_t e = launch_append(ra, aa, pool->head_dim, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return hip_fail(e, "pcr_rope_append_kv: launch");
-    return PCR_OK;
+    return launch_append(ra, aa, pool->head_dim, static_cast<hipStream_t>(stream));
 }
 
 pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, const int32_t *positions,
