@@ -385,7 +385,8 @@ pcr_status rope_args(const pcr_rope *rope, int32_t head_dim, int32_t inverse, co
 }
 
 // T rows of `width` elements at `stride` (multiples of 8 elements, 16-byte aligned).
-pcr_status check_rows(const void *x, int64_t stride, int64_t width, const char *what, const char *who)
+constexpr int64_t kMaxSpan = 1ll << 47;   // elements: all 48-bit addresses
+pcr_status check_rows(const void *x, int32_t T, int64_t stride, int64_t width, const char *what, const char *who)
 {
     if (!x) return fail(PCR_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
     if ((uintptr_t)x & 15) return fail(PCR_ERR_INVALID_ARG, "%s: %s must be 16-byte aligned", who, what);
@@ -393,6 +394,9 @@ pcr_status check_rows(const void *x, int64_t stride, int64_t width, const char *
     if (stride < width || stride % 8 || stride > (int64_t)1 << 40)
         return fail(PCR_ERR_INVALID_ARG, "%s: %s stride %lld is not a multiple of 8 of at least %lld", who, what,
                     (long long)stride, (long long)width);
+    if (stride > kMaxSpan / T)
+        return fail(PCR_ERR_UNSUPPORTED, "%s: %d rows of %s at stride %lld reach past all addresses", who, T, what,
+                    (long long)stride);
     return PCR_OK;
 }
 
@@ -400,7 +404,7 @@ bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
 {
     return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
-// From the first element of T rows to the last.
+// Bytes from the first element of T rows to the last (2^48 and a row at most: check_rows).
 int64_t span(int32_t T, int64_t stride, int64_t width) { return ((int64_t)(T - 1) * stride + width) * 2; }
 
 bool rows_overlap(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int32_t T, int64_t width)
@@ -510,10 +514,10 @@ pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, con
     if (!positions || !slot_mapping) return fail(PCR_ERR_INVALID_ARG, "%s: NULL positions or slot_mapping", who);
     if (pos_stride < T && rope->num_axes > 1)
         return fail(PCR_ERR_INVALID_ARG, "%s: pos_stride %lld < T", who, (long long)pos_stride);
-    st = check_rows(k_new, k_stride, kv_width, "k_new", who);
-    if (!st) st = check_rows(v_new, v_stride, kv_width, "v_new", who);
-    if (!st && num_q_heads > 0) st = check_rows(q, q_stride, q_width, "q", who);
-    if (!st && num_q_heads > 0) st = check_rows(q_out, q_width, q_width, "q_out", who);
+    st = check_rows(k_new, T, k_stride, kv_width, "k_new", who);
+    if (!st) st = check_rows(v_new, T, v_stride, kv_width, "v_new", who);
+    if (!st && num_q_heads > 0) st = check_rows(q, T, q_stride, q_width, "q", who);
+    if (!st && num_q_heads > 0) st = check_rows(q_out, T, q_width, q_width, "q_out", who);
     if (st) return st;
     if (num_q_heads > 0) {
         if (!(q == q_out && q_stride == q_width) && rows_overlap(q, q_stride, q_out, q_width, T, q_width))
@@ -566,8 +570,8 @@ pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, 
     if (pos_stride < T && rope->num_axes > 1)
         return fail(PCR_ERR_INVALID_ARG, "%s: pos_stride %lld < T", who, (long long)pos_stride);
     const int64_t width = (int64_t)num_heads * head_dim;
-    st = check_rows(x, x_stride, width, "x", who);
-    if (!st) st = check_rows(out, out_stride, width, "out", who);
+    st = check_rows(x, T, x_stride, width, "x", who);
+    if (!st) st = check_rows(out, T, out_stride, width, "out", who);
     if (st) return st;
     if (!(x == out && x_stride == out_stride) && rows_overlap(x, x_stride, out, out_stride, T, width))
         return fail(PCR_ERR_INVALID_ARG, "%s: x and out overlap (and are not one array)", who);

@@ -1,4 +1,5 @@
-"""CPU: what the rotations refuse because of its size alone: launches beyond 2^32 threads."""
+"""CPU: what the rotations refuse because of its size alone: launches beyond 2^32 threads, and
+rows that reach past every address, where an overlap could not be told."""
 import ctypes
 
 import numpy as np
@@ -28,3 +29,13 @@ def _append(T, Hq, Hkv, d, k_stride=None, q_stride=None):
 def test_append_grid(T, Hq, Hkv, d):
     """Q takes one thread per 16 dims of 4 heads: T * Hq (64 dims) or 2 * T * Hq of them (128)."""
     assert _append(T, Hq, Hkv, d) == UNS and "threads" in pcr.last_error()
+
+
+def test_rows_beyond_addresses():
+    for kw in (dict(k_stride=1 << 40), dict(q_stride=1 << 40)):
+        assert _append(1 << 24, 8, 2, 64, **kw) == UNS and "addresses" in pcr.last_error(), kw
+    rope = _rope(64)
+    for xs, os in ((1 << 40, 128), (128, 1 << 40), (1 << 40, 1 << 40)):
+        # out's rows lie among x's: an end that wraps around would hide it
+        assert pcr.lib().pcr_rope_rows(ctypes.addressof(rope), A, xs, 2 * A, 1 << 24, 1 << 24, 2, 64, 0, A + 4096, os,
+                                       None) == UNS and "addresses" in pcr.last_error()
