@@ -456,10 +456,10 @@ def _current_gpu():
     return torch, torch._C._cuda_getDevice() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2
 
 
-def _refuse(x, n: int, dtype: str, cur: int, what: str):
+def _refuse(x, n: int, right_type: bool, dtype: str, cur: int, what: str):
     """Says which of the conditions of a device array does not hold."""
-    if str(x.dtype) != dtype and not (dtype == "2-byte" and x.element_size() == 2):
-        raise ValueError(f"{what} holds {x.dtype}, not {dtype} elements")
+    if not right_type:
+        raise ValueError(f"{what} holds {x.dtype}, not {dtype}")
     if x.numel() < n:
         raise ValueError(f"{what} holds {x.numel()} elements, the call takes {n}")
     if x.get_device() != cur:
@@ -470,14 +470,22 @@ def _refuse(x, n: int, dtype: str, cur: int, what: str):
 def _ints(gpu, n: int, x, what: str):
     """The address of an int32 array of at least n elements on the current GPU."""
     if x.dtype is not gpu[0].int32 or x.numel() < n or x.get_device() != gpu[1] or not x.is_contiguous():
-        _refuse(x, n, "torch.int32", gpu[1], what)
+        _refuse(x, n, x.dtype is gpu[0].int32, "torch.int32 elements", gpu[1], what)
     return x.data_ptr()
 
 
+_BF16 = "2-byte bf16 elements (or their bits as 16-bit integers)"
+
+
+def _is_bf16(torch, x) -> bool:
+    """bf16 or its bits; the bits of another type of 2 bytes would be read as bf16."""
+    return x.dtype is torch.bfloat16 or x.dtype is torch.int16 or x.dtype is torch.uint16
+
+
 def _halves(gpu, n: int, x, what: str):
-    """The same of 2-byte elements."""
-    if x.element_size() != 2 or x.numel() < n or x.get_device() != gpu[1] or not x.is_contiguous():
-        _refuse(x, n, "2-byte", gpu[1], what)
+    """The same of bf16 elements."""
+    if not _is_bf16(gpu[0], x) or x.numel() < n or x.get_device() != gpu[1] or not x.is_contiguous():
+        _refuse(x, n, _is_bf16(gpu[0], x), _BF16, gpu[1], what)
     return x.data_ptr()
 
 
@@ -556,13 +564,13 @@ def _positions(gpu, positions, num_axes: int, T: int) -> int:
 
 
 def _rows(gpu, x, T: int, H: int, d: int, what: str) -> int:
-    """Checks x [T][H][d] (or [T][H*d]) of 2-byte elements, a token's heads back to back;
+    """Checks x [T][H][d] (or [T][H*d]) of bf16 elements, a token's heads back to back;
     returns the elements from one token to the next."""
     shape, st = tuple(x.shape), x.stride()
     if shape != (T, H, d) and shape != (T, H * d):
         raise ValueError(f"{what} must be [{T}][{H}][{d}], not {list(shape)}")
-    if x.element_size() != 2:
-        raise ValueError(f"{what} holds {x.dtype}, not 2-byte elements")
+    if not _is_bf16(gpu[0], x):
+        raise ValueError(f"{what} holds {x.dtype}, not {_BF16}")
     if T > 0 and (st[-1] != 1 or (len(shape) == 3 and H > 1 and st[1] != d)):
         raise ValueError(f"{what}: the heads of a token are not back to back")
     if x.get_device() != gpu[1]:
