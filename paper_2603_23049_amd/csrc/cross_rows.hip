@@ -42,6 +42,7 @@ struct CrossArgs {
     int32_t num_blocks, Hkv, Hq, max_blocks, B, T;
     int32_t cols;                 // packed rows of a sequence, at most
     int32_t steps;                // of all pairs
+    int32_t runs;
     int32_t base, rem;            // steps of a run (run_begin); even cut only
     int32_t parts;                // runs of a pair; cut by pairs only
     float scale_log2;
@@ -207,8 +208,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
     }
 }
 
-// One wave per (pair, column) of a pair cut between runs:
-// out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p with M = max_p m_p, in the parts' order.
+// out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p with M = max_p m_p, over the parts p of a pair
+// cut between runs, in their order. One wave per (pair, column) of a batch cut by pairs. In an even
+// cut one per (run from the second on, column): of a pair that is cut one run is the first to begin
+// inside it, and that run's wave merges it. So the waves are bounded by the runs, and the time
+// grows with the sequences as one scan of them does. A wave per pair, each of which sums the
+// sequences before its own, took time with their square and at 2^22 pairs of 16 columns more
+// threads than a launch has (16 / 4 heads of 64, sequences of 30-60 keys and one of 3000: 16384 of them
+// 1648 us that way, 424 this; 4096 169 and 111; 300 15.5 and 15.8; 64 ragged ones alike).
 constexpr int kCombineWaves = 4;
 template <int D, int CUT>
 __global__ __launch_bounds__(64 * kCombineWaves) void cross_rows_combine_kernel(
@@ -219,34 +226,36 @@ __global__ __launch_bounds__(64 * kCombineWaves) void cross_rows_combine_kernel(
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int task = blockIdx.x * kCombineWaves + wave;
-    const int pc = task / a.cols, c = task - pc * a.cols;
-    const int b = pc / a.Hkv, g = pc - b * a.Hkv;
-    if (b >= a.B) return;
-    int n, t0, rows;
-    const int st = pair_steps(a, key_lens, cu_q, b, n, t0, rows);
-    if (st == 0 || c >= rows) return;
+    const int nth = task / a.cols, c = task - nth * a.cols;
+    int g, t0, rows;              // kv head of the pair, first row and packed rows of its sequence
     int slot0, odd = 0, parts;    // slot of the first part (plus odd), slots from part to part, parts
     constexpr int kStride = CUT == kParts ? 1 : 2;
     if constexpr (CUT == kParts) {
+        const int b = nth / a.Hkv;
+        g = nth - b * a.Hkv;
+        if (b >= a.B) return;
+        int n;
+        const int st = pair_steps(a, key_lens, cu_q, b, n, t0, rows);
+        if (st == 0) return;
         const int per = (st + a.parts - 1) / a.parts;
         parts = (st + per - 1) / per;
-        slot0 = pc * a.parts;
+        slot0 = nth * a.parts;
     } else {
-        int sum = 0;              // steps of the sequences before
-        for (int b1 = lane; b1 < b; b1 += 64) {
-            int n1, t1, r1;
-            sum += pair_steps(a, key_lens, cu_q, b1, n1, t1, r1) * a.Hkv;
-        }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
-        const int x = sum + g * st;
-        if (x + st > a.steps) return;                   // (device lengths longer than the host's)
-        const int u0 = run_of(a, x);
-        parts = run_of(a, x + st - 1) - u0 + 1;
+        const int u0 = nth, x1 = run_begin(a, u0 + 1);   // does run u0 + 1 begin inside a pair that u0 begins?
+        At at;
+        if (u0 + 1 >= a.runs || !find_sequence(a, key_lens, cu_q, x1, at)) return;
+        if ((uint32_t)(x1 - at.first) >= (uint32_t)(at.st * a.Hkv)) return;   // (device lengths that are not the host's)
+        g = (x1 - at.first) / at.st;
+        const int x = at.first + g * at.st;              // the pair's first step
+        if (x == x1 || x < run_begin(a, u0)) return;
+        if (x + at.st > a.steps) return;                 // (device lengths longer than the host's)
+        t0 = at.t0;
+        rows = at.rows;
+        parts = run_of(a, x + at.st - 1) - u0 + 1;
         slot0 = 2 * u0;
-        odd = run_begin(a, u0) == x ? 0 : 1;            // its run's last segment, or its first
+        odd = run_begin(a, u0) == x ? 0 : 1;             // its run's last segment, or its first
     }
-    if (parts == 1) return;                             // written by its run
+    if (c >= rows || parts == 1) return;                 // (one part: written by its run)
     auto slot = [&](int p) { return (int64_t)(slot0 + kStride * p + (p == 0 ? odd : 0)) * a.cols + c; };
     float M = -INFINITY, L = 0.f, acc[E];
 #pragma unroll
@@ -367,6 +376,7 @@ hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32
     a.T = T;
     a.cols = cols;
     a.steps = (int32_t)steps;
+    a.runs = plan.runs;
     a.parts = plan.parts;
     a.base = (int32_t)(steps / plan.runs);
     a.rem = (int32_t)(steps % plan.runs);
@@ -393,7 +403,8 @@ hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || !combine) return e;
-        const int64_t tasks = (int64_t)B * pool.num_kv_heads * cols;
+        // (runs are no more than the waves resident at once: no grid comes near its limit)
+        const int64_t tasks = (plan.parts ? (int64_t)B * pool.num_kv_heads : plan.runs - 1) * cols;
         auto merge = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)((tasks + kCombineWaves - 1) / kCombineWaves)),
                                dim3(64 * kCombineWaves), 0, s, a, key_lens, cu_q, ws_o, ws_ml, oo);
