@@ -418,6 +418,9 @@ pcr_status pcr_gather_kv(const pcr_kv_pool *pool, const int32_t *block_tables, i
  *   context_lens[B]                  p_b + s_b (p_b where not served); may be prefix_lens itself
  *   free_count_out[1]                free_count less the blocks taken; may be free_count itself
  *   status[3]                        sequences served, blocks taken, tokens (cu_suffix[B])
+ * The entry points that take host copies of the lengths (attention, cross attention) need them as
+ * the device has them after this call: the caller's own lengths where it knows that every
+ * sequence fits, else with s = 0 for the sequences from status[0] on, which it reads back.
  * Otherwise the arrays must not overlap. num_blocks: blocks of the pool. The call allocates
  * nothing and may be captured into a graph; with lengths and counts updated in place each
  * replay is the next step.
@@ -537,8 +540,8 @@ pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, 
  *                    workspace serves every call ordered on one stream; calls that may
  *                    overlap (captured graphs that may run together among them) need their own.
  * Numerics as for pcr_prefix_prefill_attn; slots past n_b are never read into the result.
- * The split of the work follows from the host lengths alone, so repeated calls give
- * identical bits.
+ * The split of the work follows from the host lengths, the device's compute units and the
+ * schedule that is set, so repeated calls give identical bits.
  * Errors: as pcr_prefix_prefill_attn, PCR_ERR_UNSUPPORTED beyond 2^30 keys in a sequence or
  * 2^22 pairs of sequence and kv head, and PCR_ERR_INVALID_ARG when q and out overlap or the
  * workspace is missing, misaligned or too small (the message names the size needed).
