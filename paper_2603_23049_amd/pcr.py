@@ -544,6 +544,7 @@ class Rope:
         self._c = _Rope(self.inv_freq.ctypes.data, None if self.pair_axis is None else self.pair_axis.ctypes.data,
                         2 * self.inv_freq.size, self.num_axes, int(bool(interleaved)), float(scale))
         self._addr = ctypes.addressof(self._c)
+        self._arrays = self.inv_freq, self.pair_axis     # what _c points to
 
 
 def _positions(gpu, positions, num_axes: int, T: int) -> int:
