@@ -351,10 +351,14 @@ constexpr int64_t kRowsBytes = 4ll << 20;
 // Bytes of input above which it is read, and Q written, past the caches: input and output no
 // longer fit the 256 MB cache together. 18480 tokens as above (227 MB in) 92 -> 78 us =
 // 5.8 TB/s, with input in or out of the caches; 16384 rows of 40 heads of 128 (168 MB) 69 -> 64
-// out of them, 65 -> 63 in them. Below, 8000 tokens (98 MB) just written by the pass before
-// would take 38 instead of 34 (out of the caches 38 instead of 42). Only where each chunk's
-// wave stores whole lines (runs of 64 pairs, or more of them back to back): 8065 rows of 80 dims
-// would take 15 instead of 12 us.
+// out of them, 65 -> 63 in them. Below the line it depends on where the input is. Past the caches
+// it takes less time where the input is out of them (8000 tokens, 98 MB, 43 -> 38; 4000 24.8 -> 21.3; 4096
+// rows of 40 heads of 128 21.4 -> 16.7) and more where the pass before has just written it (33.8 ->
+// 37.9, 18.6 -> 20.2, 13.2 -> 14.2), which is how a layer's step finds its projections; 2000 tokens
+// alone gain either way (13.2 -> 10.9, 9.8 -> 8.6). Only where each chunk's wave stores whole
+// lines (runs of 64 pairs, or more of them back to back): 8065 rows of 80 dims would take 15
+// instead of 12 us out of the caches. So adjacent pairs and heads turned in part stay with the caches
+// at every size: 18480 tokens take 92 us with either.
 constexpr int64_t kNtBytes = 128ll << 20;
 bool whole_lines(const RopeArgs &ra) { return !ra.interleaved && ra.half % 64 == 0; }
 
