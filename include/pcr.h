@@ -499,7 +499,8 @@ typedef struct pcr_rope {
  *   num_q_heads      0: no Q (q and q_out are not read)
  * k_new and v_new must not overlap q_out, none of the three the pool. Errors: as pcr_append_kv;
  * PCR_ERR_INVALID_ARG for the stride, alignment, overlap and rope conditions above;
- * PCR_ERR_UNSUPPORTED beyond 2^27 tokens or 2^32 threads (about one per 16 dims of 4 query heads).
+ * PCR_ERR_UNSUPPORTED beyond 2^27 tokens, 2^32 threads (about one per 16 dims of 4 query heads)
+ * or 2^48 bytes from the first row of an array to its last.
  */
 pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, const void *q, int64_t q_stride,
                               const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
@@ -515,6 +516,7 @@ pcr_status pcr_rope_append_kv(const pcr_rope *rope, const pcr_kv_pool *pool, con
  * out may be x itself when the strides are equal, otherwise they must not overlap (with equal
  * strides they may be different parts of the same rows); both
  * 16-byte aligned, strides multiples of 8 and at least num_heads * head_dim. T = 0 is a no-op.
+ * PCR_ERR_UNSUPPORTED beyond 2^27 tokens, or 2^48 bytes from the first row of an array to its last.
  */
 pcr_status pcr_rope_rows(const pcr_rope *rope, const void *x, int64_t x_stride, const int32_t *positions,
                          int64_t pos_stride, int32_t T, int32_t num_heads, int32_t head_dim, int32_t inverse,
