@@ -561,6 +561,138 @@ pcr_status pcr_cross_attn(const void *q, const pcr_kv_pool *pool, const int32_t 
 pcr_status pcr_cross_attn_workspace_size(int32_t B, int32_t total_rows, int32_t num_q_heads, int32_t num_kv_heads,
                                          int32_t head_dim, int32_t max_keys, int64_t *bytes);
 
+/*
+ * Trees of drafted tokens: a speculative step. Sequence b's nodes are the rows
+ * cu_nodes[b] .. cu_nodes[b+1] - 1 of every array over nodes (n_b of them, numbered from 0
+ * inside the sequence). Node 0 is the last token of the text, whose K/V the pool does not hold yet; the
+ * others are drafted. parents[i] of node i is the node that it follows, 0 <= parents[i] < i, or -1:
+ * it follows the p_b cached tokens. Node k's K/V lie at logical position p_b + k (the slots that
+ * pcr_assign_blocks gives n_b new tokens), whatever its position in the text. A step in turn:
+ *   pcr_assign_blocks, pcr_draft_tree; per layer pcr_rope_append_kv (with the tree's positions)
+ *   and pcr_tree_attn; pcr_verify_drafts; pcr_compact_kv; pcr_release_blocks (lens p_b + n_b,
+ *   keep_lens the context_lens of pcr_verify_drafts).
+ * The calls allocate nothing and may be captured into a graph. cu_nodes ascends; rows from
+ * cu_nodes[B] on are neither read nor written.
+ */
+
+/*
+ * pcr_draft_tree -- what every node sees and where it stands. Bit k % 64 of word k / 64 of
+ * visible row i is set when node k of the sequence is i itself or an ancestor of it; the
+ * position is p_b plus the ancestors' count. A node whose parent is outside [-1, i), whose
+ * ancestor's is, or with i >= 64 * mask_words is not part of the tree (padding, say): no bits, position p_b.
+ *   cu_nodes[B+1], parents[T], prefix_lens[B]   device int32, read; T: rows of the arrays,
+ *                  at least cu_nodes[B]
+ *   visible        device uint64 [T][mask_words], 8-byte aligned; mask_words 1 to 16
+ *   positions      device int32 [T]
+ * No output may overlap another array. Errors: PCR_ERR_UNSUPPORTED for other mask_words, more than 2^21
+ * sequences or 2^27 nodes; PCR_ERR_INVALID_ARG for negative counts, NULL arrays, a
+ * misaligned visible.
+ */
+pcr_status pcr_draft_tree(int32_t B, const int32_t *cu_nodes, const int32_t *parents, const int32_t *prefix_lens,
+                          int32_t T, int32_t mask_words, uint64_t *visible, int32_t *positions, void *stream);
+
+/*
+ * pcr_tree_attn -- attention of a tree's rows: node i of sequence b attends the p_b cached
+ * tokens and the nodes of its visible words, keys S = [0, p_b) and p_b + k for every bit k < n_b:
+ *     out = sum_{j in S} softmax_j(sm_scale * <q, k_j>) v_j;   S empty: zeros
+ *   q, out           device bf16 [cu_nodes[B]][Hq][d], 16-byte aligned, not overlapping; fp32
+ *                    accumulation, rounded to nearest even
+ *   block_tables     device int32 [B][max_blocks]; entries past ceil((p_b + n_b)/bs) are not read;
+ *                    an id outside the pool reads block 0
+ *   prefix_lens[B], cu_nodes[B+1]   device int32, and host copies of the same (they size the
+ *                    launch and must be equal)
+ *   visible          device uint64 [cu_nodes[B]][mask_words] (pcr_draft_tree, or any other words: a
+ *                    row need not see itself), 8-byte aligned; n_b <= 64 * mask_words
+ *   workspace        as pcr_cross_attn's, of pcr_tree_attn_workspace_size bytes
+ * What a row does not see does not reach it: slots of hidden nodes and past p_b + n_b may hold
+ * anything, infinities and NaN too. Numerics as for pcr_prefix_prefill_attn. The split of the
+ * work follows from the host lengths, the device's compute units and the schedule that is set,
+ * so repeated calls give identical bits.
+ * Errors: as pcr_cross_attn; PCR_ERR_INVALID_ARG for a sequence of more than 64 * mask_words nodes;
+ * PCR_ERR_UNSUPPORTED for mask_words outside 1 .. 16 or more than 2^30 keys in a sequence.
+ */
+pcr_status pcr_tree_attn(const void *q, const pcr_kv_pool *pool, const int32_t *block_tables, int32_t max_blocks,
+                         const int32_t *prefix_lens, const int32_t *cu_nodes, const int32_t *host_prefix_lens,
+                         const int32_t *host_cu_nodes, int32_t B, const uint64_t *visible, int32_t mask_words,
+                         int32_t num_q_heads, float sm_scale, void *out, void *workspace, int64_t workspace_bytes,
+                         void *stream);
+
+/*
+ * pcr_tree_attn_workspace_size -- bytes of workspace that serve every pcr_tree_attn call on the
+ * current device of at most B sequences with at most total_nodes nodes in all and at most
+ * max_keys keys (p_b + n_b) each. PCR_ERR_HIP when no device is usable.
+ */
+pcr_status pcr_tree_attn_workspace_size(int32_t B, int32_t total_nodes, int32_t num_q_heads, int32_t num_kv_heads,
+                                        int32_t head_dim, int32_t max_keys, int64_t *bytes);
+
+/*
+ * pcr_verify_drafts -- which drafted tokens stay, and the token after them, so that the tokens
+ * of a step are distributed as the target's (speculative sampling, over a tree). The walk of
+ * sequence b starts on node u = 0. With p_u the target's distribution behind node u, q_u the one
+ * that u's drafted children were drawn from, and a = 0, Z = 1, the children of u (nodes i >= 1 with
+ * parents[i] = u) are tried in their order: with x = tokens[i] and w = max(p_u(x) - a q_u(x), 0)
+ *     uniforms[i] * q_u(x) * Z < w:  i stays, and the walk goes on from u = i, with a = 0, Z = 1;
+ *     else a becomes a + Z, and then Z = sum_v max(p_u(v) - a q_u(v), 0).
+ * Without q (draft_probs NULL) every child was proposed for certain (a draft's best tokens): w = p_u(x),
+ * or 0 if a refused child of u had the same token; it stays if uniforms[i] * Z < w, else Z
+ * becomes Z - w and x leaves the distribution. On the last node r(v) is what is left,
+ * max(p_u(v) - a q_u(v), 0), or p_u without the refused tokens; with S = sum r the next token is the
+ * least v with r(0) + .. + r(v) > uniforms[0] * S (the last v with r(v) > 0 if rounding leaves
+ * none). If S = 0, r = p_u takes its place. The walk ends too once path_cap nodes stay.
+ *   cu_nodes[B+1], parents[T], tokens[T], prefix_lens[B]   device int32, read; T as for
+ *                  pcr_draft_tree. A token outside [0, vocab) never stays and refuses nothing.
+ *   target_probs   device fp32: row t (node t's) at t * target_stride elements, vocab of them;
+ *   draft_probs    likewise, or NULL; row t is read only where a child of node t is tried
+ *   uniforms       device fp32 [T], in [0, 1)
+ *   path           device int32 [B][path_cap], written: the nodes that stay, node 0 first, -1 after
+ *   accepted_lens  device int32 [B]: how many (1 + the drafted tokens that stay; 0 if n_b = 0)
+ *   next_tokens    device int32 [B]: the drawn token, -1 if n_b = 0
+ *   context_lens   device int32 [B]: prefix_lens[b] + accepted_lens[b]; may be prefix_lens itself
+ *   workspace      device memory owned by the caller, 16-byte aligned, of
+ *                  pcr_verify_drafts_workspace_size bytes (NULL when that is 0); scratch. One
+ *                  workspace serves every call ordered on one stream; calls that may overlap
+ *                  (captured graphs that may run together among them) need their own.
+ * Probabilities that are negative or NaN count as 0; rows need not sum to one exactly. Sums are
+ * fp64, products and differences rounded one by one, in an order that is fixed for a given B and vocab:
+ * repeated calls give the same tokens. No other overlap of outputs. Errors: PCR_ERR_INVALID_ARG for
+ * negative counts, vocab or path_cap < 1, strides below vocab, NULL arrays, a workspace that is
+ * missing, misaligned or too small; PCR_ERR_UNSUPPORTED beyond 2^21 sequences, 2^27 nodes, a
+ * vocabulary of 2^30 or strides of 2^32.
+ */
+pcr_status pcr_verify_drafts(int32_t B, const int32_t *cu_nodes, const int32_t *parents, const int32_t *tokens,
+                             int32_t T, int32_t vocab, const float *target_probs, int64_t target_stride,
+                             const float *draft_probs, int64_t draft_stride, const float *uniforms,
+                             const int32_t *prefix_lens, int32_t path_cap, int32_t *path, int32_t *accepted_lens,
+                             int32_t *next_tokens, int32_t *context_lens, void *workspace, int64_t workspace_bytes,
+                             void *stream);
+
+/*
+ * pcr_verify_drafts_workspace_size -- bytes of workspace that serve every pcr_verify_drafts call on
+ * the current device of at most B sequences with at most T rows and this vocabulary.
+ */
+pcr_status pcr_verify_drafts_workspace_size(int32_t B, int32_t T, int32_t vocab, int64_t *bytes);
+
+/*
+ * pcr_compact_kv -- moves the nodes that stay into consecutive slots, in every layer: for i <
+ * accepted_lens[b], the K/V at logical position p_b + path[b][i] go to position p_b + i (bitwise; as
+ * if all were read before any is written). What lay there, and the slots behind the kept
+ * tokens, are then free for other tokens (pcr_release_blocks hands whole blocks back).
+ *   pools          host array of n_layers pools of one shape; their K and V arrays must all be
+ *                  apart. Read during the call only.
+ *   block_tables   device int32 [B][max_blocks]; the blocks from position p_b on belong to b alone
+ *   prefix_lens[B], path[B][path_cap], accepted_lens[B]   device int32 (pcr_verify_drafts);
+ *                  an accepted_lens beyond path_cap counts as path_cap
+ * A path is strictly ascending from 0 or above, as every way down a tree is. The moves of a
+ * sequence end before the first entry that is not, whose position is past the table's row, or whose
+ * block is outside the pool; none are made for a negative prefix.
+ * Errors: as pcr_append_kv for each pool; PCR_ERR_INVALID_ARG for negative counts, pools of
+ * different shapes or that overlap, max_blocks or path_cap < 1, NULL arrays; PCR_ERR_UNSUPPORTED beyond
+ * 256 layers, 65535 sequences or 2^27 blocks. n_layers = 0 or B = 0 is a no-op.
+ */
+pcr_status pcr_compact_kv(const pcr_kv_pool *pools, int32_t n_layers, const int32_t *block_tables, int32_t max_blocks,
+                          const int32_t *prefix_lens, const int32_t *path, int32_t path_cap,
+                          const int32_t *accepted_lens, int32_t B, void *stream);
+
 /* Per-layer device inputs and outputs for pcr_pipeline_run. */
 typedef struct pcr_layer_io {
     pcr_host_kv host;     /* this layer's pinned host store */

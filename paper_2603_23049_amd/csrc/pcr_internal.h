@@ -112,6 +112,12 @@ hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32
                              const int32_t *key_lens, const int32_t *cu_q, int32_t B, int32_t num_q_heads, int32_t T,
                              int32_t cols, int64_t steps, const CrossRowsPlan &plan, bool combine, float sm_scale,
                              void *out, void *workspace, hipStream_t s);
+// Trees of drafted tokens (draft.hip, verify.hip, tree.hip).
+constexpr int32_t kMaxMaskWords = 16;        // 64-bit words of a node's visible set
+constexpr int32_t kMaxTreeSeqs = 1 << 21;    // a workgroup of up to 1024 threads each: below 2^32 threads
+constexpr int32_t kMaxTreeNodes = 1 << 27;
+constexpr int32_t kMaxVocab = 1 << 30;
+constexpr int64_t kMaxRowStride = (int64_t)1 << 32;   // elements; times the rows, below 2^62 bytes
 // Size of the allocation-free decode entry point's per-device scratch (decode.hip),
 // and its device address on the current device (taken with hipGetSymbolAddress on the
 // first call per device, then reused).

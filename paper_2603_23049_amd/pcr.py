@@ -39,7 +39,8 @@ EXPORTS = ["pcr_plan", "pcr_plan_offload", "pcr_load_kv_layer", "pcr_load_kv_lay
            "pcr_load_kv_layer_staged", "pcr_append_kv",
            "pcr_prefix_prefill_attn", "pcr_prefill_attn_set_schedule", "pcr_prefill_attn_hold_scratch", "pcr_decode_attn", "pcr_decode_attn_noalloc", "pcr_decode_attn_workspace_size", "pcr_gather_kv", "pcr_pipeline_run", "pcr_pipeline_run_staged",
            "pcr_assign_blocks", "pcr_release_blocks", "pcr_rope_append_kv", "pcr_rope_rows", "pcr_cross_attn",
-           "pcr_cross_attn_workspace_size",
+           "pcr_cross_attn_workspace_size", "pcr_draft_tree", "pcr_tree_attn", "pcr_tree_attn_workspace_size",
+           "pcr_verify_drafts", "pcr_verify_drafts_workspace_size", "pcr_compact_kv",
            "pcr_pipeline_run_offload", "pcr_pipeline_run_offload_staged",
            "pcr_store_open", "pcr_store_write_async", "pcr_store_read_async", "pcr_store_wait",
            "pcr_store_poll", "pcr_store_stats", "pcr_store_close", "pcr_last_error", "pcr_version"]
@@ -114,6 +115,13 @@ def lib():
         L.pcr_cross_attn.argtypes = [P, ctypes.POINTER(_Pool), P, i32, P, P, P, P, i32, i32, ctypes.c_float, P, P,
                                      i64, P]
         L.pcr_cross_attn_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
+        L.pcr_draft_tree.argtypes = [i32, P, P, P, i32, i32, P, P, P]
+        L.pcr_tree_attn.argtypes = [P, ctypes.POINTER(_Pool), P, i32, P, P, P, P, i32, P, i32, i32, ctypes.c_float, P,
+                                    P, i64, P]
+        L.pcr_tree_attn_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
+        L.pcr_verify_drafts.argtypes = [i32, P, P, P, i32, i32, P, i64, P, i64, P, P, i32, P, P, P, P, P, i64, P]
+        L.pcr_verify_drafts_workspace_size.argtypes = [i32, i32, i32, ctypes.POINTER(i64)]
+        L.pcr_compact_kv.argtypes = [P, i32, P, i32, P, P, i32, P, i32, P]
         L.pcr_pipeline_run.argtypes = [ctypes.POINTER(_LayerIO), i32, ctypes.POINTER(_Batch), ctypes.c_int, P, P,
                                        P]
         L.pcr_pipeline_run_staged.argtypes = [ctypes.POINTER(_LayerIO), i32, ctypes.POINTER(_Batch), P, i64, P, P,
@@ -607,6 +615,30 @@ def rope_rows(rope: Rope, x, positions, out, inverse: bool = False, stream=None)
                                out.data_ptr(), os_, _stream(stream)))
 
 
+def _new_workspace(n: int, device, stream):
+    """n bytes of device memory in the order of the call's stream (None if there are none)."""
+    if n == 0:
+        return None
+    import torch
+    if stream is None:
+        s = torch.cuda.current_stream(device)
+    elif isinstance(stream, int):
+        s = torch.cuda.ExternalStream(stream, device=device)
+    else:
+        s = stream
+    with torch.cuda.stream(s):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _workspace(gpu, workspace):
+    """Its address and bytes (None, 0 without one)."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != gpu[1] or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the current GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def cross_attn_workspace_bytes(B: int, total_rows: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
                                max_keys: int) -> int:
     """pcr_cross_attn_workspace_size on the current device."""
@@ -633,25 +665,144 @@ def cross_attn(q, pool: KVPool, block_tables, key_lens, cu_q, host_key_lens, hos
     klp, cup = _ints(gpu, B, key_lens, "key_lens"), _ints(gpu, B + 1, cu_q, "cu_q")
     p = _pool_here(gpu, pool)
     if workspace is None and T > 0:
-        n = cross_attn_workspace_bytes(B, T, Hq, pool.num_kv_heads, d, int(hkl.max()))
-        if n > 0:
-            import torch
-            if stream is None:
-                s = torch.cuda.current_stream(q.device)
-            elif isinstance(stream, int):
-                s = torch.cuda.ExternalStream(stream, device=q.device)
-            else:
-                s = stream
-            with torch.cuda.stream(s):
-                workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
-    wsp, ws_bytes = None, 0
-    if workspace is not None:
-        ws_bytes = workspace.numel() * workspace.element_size()
-        if workspace.get_device() != gpu[1] or not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous and on the current GPU")
-        wsp = workspace.data_ptr()
+        workspace = _new_workspace(cross_attn_workspace_bytes(B, T, Hq, pool.num_kv_heads, d, int(hkl.max())), q.device,
+                                   stream)
+    wsp, ws_bytes = _workspace(gpu, workspace)
     _check(lib().pcr_cross_attn(qp, ctypes.byref(p), btp, mb, klp, cup, _ptr(hkl), _ptr(hcu), B, Hq, sm_scale, op, wsp,
                                 ws_bytes, _stream(stream)))
+
+
+def _words(gpu, T: int, x, what: str):
+    """Checks x [T or more][words] of 64-bit words; returns their address and the words of a row."""
+    if x.dtype is not gpu[0].int64 and x.dtype is not gpu[0].uint64:
+        raise ValueError(f"{what} holds {x.dtype}, not 64-bit words (torch.int64 or torch.uint64)")
+    if x.dim() != 2 or x.shape[0] < T:
+        raise ValueError(f"{what} must be [{T}][words], not {list(x.shape)}")
+    if x.get_device() != gpu[1] or not x.is_contiguous():
+        _refuse(x, 0, True, "", gpu[1], what)
+    return x.data_ptr(), x.shape[1]
+
+
+def draft_tree(cu_nodes, parents, prefix_lens, visible, positions, stream=None):
+    """pcr_draft_tree: cu_nodes [B+1], parents [T], prefix_lens [B], positions [T] int32, visible
+    [T][words] 64-bit words (torch.int64 or torch.uint64), device tensors."""
+    B, T, gpu = prefix_lens.shape[0], parents.shape[0], _current_gpu()
+    vp, words = _words(gpu, T, visible, "visible")
+    _check(lib().pcr_draft_tree(B, _ints(gpu, B + 1, cu_nodes, "cu_nodes"), _ints(gpu, T, parents, "parents"),
+                                _ints(gpu, B, prefix_lens, "prefix_lens"), T, words, vp,
+                                _ints(gpu, T, positions, "positions"), _stream(stream)))
+
+
+def tree_attn_workspace_bytes(B: int, total_nodes: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
+                              max_keys: int) -> int:
+    """pcr_tree_attn_workspace_size on the current device."""
+    n = ctypes.c_int64(0)
+    _check(lib().pcr_tree_attn_workspace_size(int(B), int(total_nodes), int(num_q_heads), int(num_kv_heads),
+                                              int(head_dim), int(max_keys), ctypes.byref(n)))
+    return int(n.value)
+
+
+def tree_attn(q, pool: KVPool, block_tables, prefix_lens, cu_nodes, host_prefix_lens, host_cu_nodes, visible,
+              num_q_heads: int, out, workspace=None, sm_scale: Optional[float] = None, stream=None):
+    """pcr_tree_attn. q/out [T][Hq][d], block_tables [B][max_blocks], prefix_lens [B], cu_nodes [B+1],
+    visible [T][words] on the device; host_* are the host copies of the lengths. Without a
+    workspace one of the needed size is allocated as decode_attn does."""
+    hpl, hcu = _i32_host(host_prefix_lens), _i32_host(host_cu_nodes)
+    B, d, Hq = int(hpl.shape[0]), pool.head_dim, int(num_q_heads)
+    if hcu.shape[0] != B + 1:
+        raise ValueError("host_cu_nodes must have B+1 entries")
+    if block_tables.dim() != 2:
+        raise ValueError("block_tables must be [B][max_blocks]")
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(d)
+    T, mb, gpu = int(hcu[-1]), block_tables.shape[1], _current_gpu()
+    qp, op = _halves(gpu, T * Hq * d, q, "q"), _halves(gpu, T * Hq * d, out, "out")
+    btp = _ints(gpu, B * mb, block_tables, "block_tables")
+    plp, cup = _ints(gpu, B, prefix_lens, "prefix_lens"), _ints(gpu, B + 1, cu_nodes, "cu_nodes")
+    vp, words = _words(gpu, T, visible, "visible")
+    p = _pool_here(gpu, pool)
+    if workspace is None and T > 0:
+        most = int((hpl.astype(np.int64) + np.diff(hcu)).max())
+        workspace = _new_workspace(tree_attn_workspace_bytes(B, T, Hq, pool.num_kv_heads, d, min(most, 2 ** 31 - 1)),
+                                   q.device, stream)
+    wsp, ws_bytes = _workspace(gpu, workspace)
+    _check(lib().pcr_tree_attn(qp, ctypes.byref(p), btp, mb, plp, cup, _ptr(hpl), _ptr(hcu), B, vp, words, Hq,
+                               sm_scale, op, wsp, ws_bytes, _stream(stream)))
+
+
+def verify_drafts_workspace_bytes(B: int, T: int, vocab: int) -> int:
+    """pcr_verify_drafts_workspace_size on the current device."""
+    n = ctypes.c_int64(0)
+    _check(lib().pcr_verify_drafts_workspace_size(int(B), int(T), int(vocab), ctypes.byref(n)))
+    return int(n.value)
+
+
+def _probabilities(gpu, x, T: int, V: int, what: str):
+    """Checks x [T or more][V] of float32, a row's elements back to back; returns its address and
+    the elements from one row to the next."""
+    if x.dtype is not gpu[0].float32:
+        raise ValueError(f"{what} holds {x.dtype}, not torch.float32")
+    if x.dim() != 2 or x.shape[0] < T or x.shape[1] != V:
+        raise ValueError(f"{what} must be [{T}][{V}], not {list(x.shape)}")
+    st = x.stride()
+    if (V > 1 and st[1] != 1) or (T > 1 and st[0] < V):
+        raise ValueError(f"{what}: the elements of a row are not back to back")
+    if x.get_device() != gpu[1]:
+        raise ValueError(f"{what} is on {x.device}, not on the current GPU")
+    return x.data_ptr(), st[0] if T > 1 else V
+
+
+def verify_drafts(cu_nodes, parents, tokens, target_probs, draft_probs, uniforms, prefix_lens, path, accepted_lens,
+                  next_tokens, context_lens, workspace=None, stream=None):
+    """pcr_verify_drafts: cu_nodes [B+1], parents and tokens [T], prefix_lens, accepted_lens,
+    next_tokens and context_lens [B], path [B][path_cap] int32; target_probs and draft_probs (or
+    None) [T][vocab] float32 with any row stride, uniforms [T] float32; device tensors. context_lens may
+    be prefix_lens. Without a workspace one of the needed size is allocated as decode_attn does."""
+    B, T, gpu = prefix_lens.shape[0], parents.shape[0], _current_gpu()
+    if target_probs.dim() != 2 or path.dim() != 2:
+        raise ValueError("target_probs must be [T][vocab], path [B][path_cap]")
+    V, cap = target_probs.shape[1], path.shape[1]
+    tp, ts = _probabilities(gpu, target_probs, T, V, "target_probs")
+    dp, ds = (None, 0) if draft_probs is None else _probabilities(gpu, draft_probs, T, V, "draft_probs")
+    if uniforms.dtype is not gpu[0].float32 or uniforms.numel() < T or uniforms.get_device() != gpu[1] or \
+            not uniforms.is_contiguous():
+        _refuse(uniforms, T, uniforms.dtype is gpu[0].float32, "torch.float32 elements", gpu[1], "uniforms")
+    args = [_ints(gpu, n, x, what) for n, x, what in (
+        (B + 1, cu_nodes, "cu_nodes"), (T, parents, "parents"), (T, tokens, "tokens"), (B, prefix_lens, "prefix_lens"),
+        (B * cap, path, "path"), (B, accepted_lens, "accepted_lens"), (B, next_tokens, "next_tokens"),
+        (B, context_lens, "context_lens"))]
+    if workspace is None and B > 0:
+        workspace = _new_workspace(verify_drafts_workspace_bytes(B, T, V), target_probs.device, stream)
+    wsp, ws_bytes = _workspace(gpu, workspace)
+    _check(lib().pcr_verify_drafts(B, args[0], args[1], args[2], T, V, tp, ts, dp, ds, uniforms.data_ptr(), args[3], cap,
+                                   args[4], args[5], args[6], args[7], wsp, ws_bytes, _stream(stream)))
+
+
+class KVLayers:
+    """The pools of a model's layers (KVPool each, of one shape), for the calls that take them all."""
+
+    def __init__(self, pools: Sequence[KVPool]):
+        self.pools = list(pools)
+        gpu = _current_gpu()
+        self._c = (_Pool * max(1, len(self.pools)))(*[_pool_here(gpu, p) for p in self.pools])
+        self._addr, self._gpu = ctypes.addressof(self._c), gpu[1]
+
+    def __len__(self):
+        return len(self.pools)
+
+
+def compact_kv(layers: KVLayers, block_tables, prefix_lens, path, accepted_lens, stream=None):
+    """pcr_compact_kv: block_tables [B][max_blocks], prefix_lens and accepted_lens [B], path
+    [B][path_cap], int32 device tensors."""
+    B, gpu = prefix_lens.shape[0], _current_gpu()
+    if block_tables.dim() != 2 or path.dim() != 2:
+        raise ValueError("block_tables must be [B][max_blocks], path [B][path_cap]")
+    if layers._gpu != gpu[1]:
+        raise ValueError("the layers' pools are not on the current GPU")
+    mb, cap = block_tables.shape[1], path.shape[1]
+    _check(lib().pcr_compact_kv(layers._addr, len(layers.pools), _ints(gpu, B * mb, block_tables, "block_tables"), mb,
+                                _ints(gpu, B, prefix_lens, "prefix_lens"), _ints(gpu, B * cap, path, "path"), cap,
+                                _ints(gpu, B, accepted_lens, "accepted_lens"), B, _stream(stream)))
 
 
 @dataclass
