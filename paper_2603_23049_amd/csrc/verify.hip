@@ -9,6 +9,12 @@
 // next Z. A draft without probabilities proposes each token for certain (q is 1 there): a refusal
 // takes the token out of p, and Z falls by its share without a pass. Sums are in 64 bits: a
 // row's cumulated sum decides between neighbouring tokens.
+//
+// The passes read all there is to read, so they are what has to fill the device: a round is a launch in
+// which several workgroups per sequence each walk as far as the walk goes without a new sum (the
+// walk itself is a few dependent loads) and then sum their tiles of the row it needs. The last
+// launch, one workgroup per sequence, ends the walk (with passes of its own where a walk needs more
+// rounds than were launched) and draws: the tile sums lead to the tile, which is read once more.
 #include <algorithm>
 
 #include "pcr_internal.h"
@@ -16,19 +22,37 @@
 namespace pcr {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));   // rows start anywhere
+
+constexpr int kRoundThreads = 256;
+constexpr int kRoundWaves = kRoundThreads / 64;
+constexpr int kFinalThreads = 1024;
+constexpr int kPiece = 1024;             // elements of a tile, times VerifyArgs::pieces; a wave sums a tile
+constexpr int kVecs = kPiece / 256;      // vectors of four of a lane and piece
+constexpr int kMaxTiles = 4096;
+
+// Where a walk stands between launches.
+enum Need { kNextZ, kSum, kNothing };    // a pass for Z, for the sum of the last row, or its tile sums are there
+struct State {
+    double a, Z;
+    int32_t at, next;                    // node, and the first node not tried yet
+    int32_t kept, need;
+    int32_t buf, fresh;                  // where the tile sums are, and whether they are those of (at, a)
+};
 
 struct VerifyArgs {
     const int32_t *cu_nodes, *parents, *tokens, *prefix_lens;
     const float *target, *draft, *uniforms;
     int64_t target_stride, draft_stride;
     int32_t *path, *accepted_lens, *next_tokens, *context_lens;
-    int32_t T, V, path_cap;
+    int32_t B, T, V, path_cap;
+    int32_t tiles, pieces, rounds;
+    State *states;                       // [2][B]
+    double *sums;                        // [2][B][tiles]
 };
 
-// What is left of a row. (The product and the difference are rounded each by itself: a fused one would
-// leave other residues where p and q are equal.)
+// What is left of a row's element. (The product and the difference are rounded each by itself: a fused
+// one would leave other residues where p and q are equal.)
 __device__ __forceinline__ double left(float p, float q, double a)
 {
 #pragma clang fp contract(off)
@@ -44,125 +68,406 @@ __device__ __forceinline__ double wave_sum(double x)
     return x;
 }
 
-// One workgroup per sequence.
-__global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a)
+__device__ __forceinline__ float lane_of(float x, int l)
 {
-    __shared__ double part[kWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x;
-    const int32_t t0 = min(max(a.cu_nodes[b], 0), a.T), n = min(a.cu_nodes[b + 1], a.T) - t0;
-    int32_t *path = a.path + (int64_t)b * a.path_cap;
-    const int32_t *parents = a.parents + t0, *tokens = a.tokens + t0;
-    int32_t at = 0, kept = n > 0 ? 1 : 0, refused = 0;      // the walk's node; refused children of it (their last)
-    double shift = 0.0, Z = 1.0;
-    const float *p = a.target + (int64_t)t0 * a.target_stride;
-    const float *q = a.draft ? a.draft + (int64_t)t0 * a.draft_stride : nullptr;
-    // Tokens of the refused children are out of the row (a draft without probabilities).
-    auto out = [&](int32_t v) {
-        for (int32_t i = at + 1; i <= refused; ++i)
-            if (parents[i] == at && tokens[i] == v) return true;
-        return false;
-    };
-    auto value = [&](int32_t v) -> double {
-        if (q) return left(p[v], q[v], shift);
-        const double r = left(p[v], 0.f, 0.0);
-        return refused > at && r > 0.0 && out(v) ? 0.0 : r;
-    };
-    auto total = [&](int32_t lo, int32_t hi) -> double {    // sum of [lo, hi), on all threads
-        double s = 0.0;
-        for (int32_t v = lo + tid; v < hi; v += kThreads) s += value(v);
-        s = wave_sum(s);
-        __syncthreads();
-        if (lane == 0) part[wave] = s;
-        __syncthreads();
-        s = 0.0;
-        for (int w = 0; w < kWaves; ++w) s += part[w];
-        return s;
-    };
-    if (tid == 0 && n > 0) path[0] = 0;
-    for (int32_t i = 1; i < n && kept < a.path_cap; ++i) {
-        if (parents[i] != at) continue;
-        const int32_t x = tokens[i];
-        if ((uint32_t)x >= (uint32_t)a.V) continue;         // no token: never kept, nothing refused
-        const double u = (double)a.uniforms[t0 + i];
-        const double w = value(x);
-        const bool yes = q ? u * (double)q[x] * Z < w : u * Z < w;
-        if (yes) {
-            at = refused = i;
-            if (tid == 0) path[kept] = i;
-            ++kept;
-            shift = 0.0;
-            Z = 1.0;
-            p = a.target + (int64_t)(t0 + i) * a.target_stride;
-            if (q) q = a.draft + (int64_t)(t0 + i) * a.draft_stride;
-        } else {
-            refused = i;
-            if (q) {
-                shift += Z;
-                Z = total(0, a.V);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
+}
+
+// A sequence's part of the arrays.
+struct Seq {
+    int32_t t0, n;
+    const int32_t *parents, *tokens;
+    const float *uniforms;
+    int32_t *path;
+};
+__device__ __forceinline__ Seq sequence(const VerifyArgs &a, int b)
+{
+    Seq s;
+    s.t0 = min(max(a.cu_nodes[b], 0), a.T);
+    s.n = max(min(a.cu_nodes[b + 1], a.T) - s.t0, 0);
+    s.parents = a.parents + s.t0;
+    s.tokens = a.tokens + s.t0;
+    s.uniforms = a.uniforms + s.t0;
+    s.path = a.path + (int64_t)b * a.path_cap;
+    return s;
+}
+
+// Goes on with a walk until it needs a sum (all lanes of one wave; the state is the same in each). Children
+// are tried in ascending order and follow their parents, so one pass over the nodes does: 64 at a
+// time, with the elements of the rows that their tests need.
+__device__ __forceinline__ void walk(const VerifyArgs &a, const Seq &s, State &st, bool lead)
+{
+    const int lane = threadIdx.x & 63;
+    while (st.next < s.n && st.kept < a.path_cap) {
+        const int32_t c0 = st.next & ~63, i = c0 + lane;
+        const bool in = i < s.n;
+        const int32_t parent = in ? s.parents[i] : -1, x = in ? s.tokens[i] : -1;
+        const float u = in ? s.uniforms[i] : 0.f;
+        const bool ok = parent >= 0 && parent < i && (uint32_t)x < (uint32_t)a.V;   // else never kept, and refuses nothing
+        float p = 0.f, q = 0.f;
+        if (__builtin_amdgcn_ballot_w64(ok && i >= st.next && parent == st.at) && ok) {   // (some child here)
+            p = a.target[(int64_t)(s.t0 + parent) * a.target_stride + x];
+            if (a.draft) q = a.draft[(int64_t)(s.t0 + parent) * a.draft_stride + x];
+        }
+        while (st.kept < a.path_cap) {
+            const uint64_t children = __builtin_amdgcn_ballot_w64(ok && i >= st.next && parent == st.at);
+            if (!children) break;
+            const int l = (int)__builtin_ctzll(children);
+            const double ul = lane_of(u, l);
+            const float pl = lane_of(p, l), ql = lane_of(q, l);
+            double w = left(pl, ql, st.a);
+            if (!a.draft) {                     // 0 where a refused child had the same token
+                const int32_t xl = __builtin_amdgcn_readlane(x, l);
+                uint64_t again = __builtin_amdgcn_ballot_w64(ok && lane < l && parent == st.at && x == xl);
+                for (int32_t j0 = st.at + 1; j0 < c0; j0 += 64) {
+                    const int32_t j = j0 + lane;
+                    again |= __builtin_amdgcn_ballot_w64(j < c0 && s.parents[j] == st.at && s.tokens[j] == xl);
+                }
+                w = again ? 0.0 : w;
+            }
+            const bool stays = (a.draft ? ul * (double)ql * st.Z : ul * st.Z) < w;
+            st.next = c0 + l + 1;
+            if (stays) {
+                st.at = c0 + l;
+                if (lead && lane == 0) s.path[st.kept] = st.at;
+                ++st.kept;
+                st.a = 0.0;
+                st.Z = 1.0;
+                st.fresh = 0;
+            } else if (a.draft) {
+                st.a += st.Z;
+                st.need = kNextZ;
+                return;
             } else {
-                Z -= w;
+                st.Z -= w;
             }
         }
+        if (st.kept >= a.path_cap) break;
+        st.next = c0 + 64;
     }
-    if (tid == 0) {
-        a.accepted_lens[b] = kept;
-        a.context_lens[b] = a.prefix_lens[b] + kept;
-    }
-    for (int32_t i = kept + tid; i < a.path_cap; i += kThreads) path[i] = -1;
-    if (n <= 0) {
-        if (tid == 0) a.next_tokens[b] = -1;
-        return;
-    }
-    // The draw: the first token whose cumulated sum passes u * S. Waves take one part of the row each.
-    double S = total(0, a.V);
-    if (!(S > 0.0)) {                                       // nothing is left: the target's own row
-        q = nullptr;
-        refused = at;
-        S = total(0, a.V);
-    }
-    double t = (double)a.uniforms[t0] * S;
-    int32_t lo = 0, hi = a.V;
-    while (hi - lo > 64) {                                  // sixteen parts of [lo, hi): the one that holds t
-        const int32_t size = ((hi - lo + kWaves - 1) / kWaves + 63) / 64 * 64;
-        const int32_t w0 = min(lo + wave * size, hi), w1 = min(w0 + size, hi);
-        double s = 0.0;
-        for (int32_t v = w0 + lane; v < w1; v += 64) s += value(v);
-        s = wave_sum(s);
-        __syncthreads();
-        if (lane == 0) part[wave] = s;
-        __syncthreads();
-        double cum = 0.0, before = 0.0;
-        int pick = -1;
-        for (int w = 0; w < kWaves && pick < 0; ++w) {
-            if (cum + part[w] > t) {
-                pick = w;
-                before = cum;
-            }
-            cum += part[w];
-        }
-        for (int w = kWaves - 1; w >= 0 && pick < 0; --w)   // (rounding: the last part with anything)
-            if (part[w] > 0.0) {
-                pick = w;
-                before = -1e300;                            // its last token, below
-            }
-        pick = max(pick, 0);
-        t = before == -1e300 ? 1e300 : t - before;
-        lo = min(lo + pick * size, hi);
-        hi = min(lo + size, hi);
-    }
-    if (wave == 0) {
-        const double r = lo + lane < hi ? value(lo + lane) : 0.0;
-        double c = r;
+    st.need = st.fresh ? kNothing : kSum;
+}
+
+// What a pass reads.
+struct Row {
+    const float *p, *q;
+    double a;
+    const int32_t *parents, *tokens;     // of the refused tokens that are out of p, if any: children of `at`
+    int32_t at, end;                     // among the nodes (at, end)
+    int32_t out0;                        // this lane's of the first 64 of them (-1: none)
+};
+__device__ __forceinline__ int32_t refused(const Row &r, int32_t j)
+{
+    return j < r.end && r.parents[j] == r.at ? r.tokens[j] : -1;
+}
+__device__ __forceinline__ Row row_of(const VerifyArgs &a, const Seq &s, const State &st)
+{
+    Row r;
+    r.p = a.target + (int64_t)(s.t0 + st.at) * a.target_stride;
+    r.q = a.draft && st.a != 0.0 ? a.draft + (int64_t)(s.t0 + st.at) * a.draft_stride : nullptr;
+    r.a = st.a;
+    r.parents = s.parents;
+    r.tokens = s.tokens;
+    r.at = st.at;
+    r.end = a.draft ? st.at + 1 : min(st.next, s.n);
+    r.out0 = refused(r, st.at + 1 + (int32_t)(threadIdx.x & 63));
+    return r;
+}
+
+// The four elements at v of the rows.
+struct Four {
+    f32x4u p, q;
+};
+__device__ __forceinline__ Four load(const Row &r, int32_t V, int32_t v)
+{
+    Four x{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if (v + 3 < V) {
+        x.p = *reinterpret_cast<const f32x4u *>(r.p + v);
+        if (r.q) x.q = *reinterpret_cast<const f32x4u *>(r.q + v);
+    } else {
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const double o = __shfl_up(c, off);
-            if (lane >= off) c += o;
-        }
-        const uint64_t over = __builtin_amdgcn_ballot_w64(c > t), some = __builtin_amdgcn_ballot_w64(r > 0.0);
-        const int32_t end = some ? 63 - (int)__builtin_clzll(some) : 0;   // the last with anything
-        const int32_t l = over ? min((int32_t)__builtin_ctzll(over), end) : end;
-        if (lane == 0) a.next_tokens[b] = lo + l;
+        for (int k = 0; k < 4; ++k)
+            if (v + k < V) {
+                x.p[k] = r.p[v + k];
+                if (r.q) x.q[k] = r.q[v + k];
+            }
     }
+    return x;
+}
+
+// What is left of them (0 from hi on); base: of the wave's first lane.
+__device__ __forceinline__ void values(const Row &r, const Four &x, int32_t base, int32_t v, int32_t hi, double (&e)[4])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = v + k < hi ? left(x.p[k], x.q[k], r.a) : 0.0;
+    // Refused tokens: 64 nodes at a time, those among the wave's 256 elements.
+    for (int32_t j0 = r.at + 1; j0 < r.end; j0 += 64) {
+        const int32_t y = j0 == r.at + 1 ? r.out0 : refused(r, j0 + (int32_t)(threadIdx.x & 63));
+        uint64_t hits = __builtin_amdgcn_ballot_w64(y >= base && y - base < 256);
+        while (hits) {
+            const int32_t at = __builtin_amdgcn_readlane(y, (int)__builtin_ctzll(hits)) - v;
+            hits &= hits - 1;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e[k] = at == k ? 0.0 : e[k];
+        }
+    }
+}
+
+// A wave's share of a pass: the tiles first, first + step, .. in pieces; AHEAD: the next one's loads in flight
+// while one is added.
+template <bool AHEAD>
+__device__ __forceinline__ void tile_sums(const VerifyArgs &a, const Row &r, int32_t first, int32_t step, double *sums)
+{
+    if (first >= a.tiles) return;
+    const int lane = threadIdx.x & 63;
+    auto begin = [&](int32_t t, int32_t piece) {            // (past the row's end: no element of it)
+        return (int32_t)min(((int64_t)t * a.pieces + piece) * kPiece, (int64_t)a.V);
+    };
+    Four x[kVecs], y[kVecs];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) x[k] = load(r, a.V, begin(first, 0) + k * 256 + 4 * lane);
+    double s = 0.0;
+    for (int32_t t = first, piece = 0; t < a.tiles;) {
+        const int32_t base = begin(t, piece);
+        const bool ends = piece + 1 == a.pieces;
+        const int32_t t2 = ends ? t + step : t, piece2 = ends ? 0 : piece + 1;
+        if (AHEAD && t2 < a.tiles) {
+#pragma unroll
+            for (int k = 0; k < kVecs; ++k) y[k] = load(r, a.V, begin(t2, piece2) + k * 256 + 4 * lane);
+        }
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            double e[4];
+            values(r, x[k], base + k * 256, base + k * 256 + 4 * lane, a.V, e);
+            s += (e[0] + e[1]) + (e[2] + e[3]);
+        }
+        if (ends) {
+            s = wave_sum(s);
+            if (lane == 0) sums[t] = s;
+            s = 0.0;
+        }
+        if (!AHEAD && t2 < a.tiles) {
+#pragma unroll
+            for (int k = 0; k < kVecs; ++k) y[k] = load(r, a.V, begin(t2, piece2) + k * 256 + 4 * lane);
+        }
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) x[k] = y[k];
+        t = t2;
+        piece = piece2;
+    }
+}
+
+// Sum of all tiles, in one order whoever adds them.
+__device__ __forceinline__ double add_tiles(const double *sums, int32_t tiles)
+{
+    double s = 0.0;
+    for (int32_t t = threadIdx.x & 63; t < tiles; t += 64) s += sums[t];
+    return wave_sum(s);
+}
+
+__device__ __forceinline__ State start(const Seq &s, bool lead)
+{
+    State st{0.0, 1.0, 0, 1, s.n > 0 ? 1 : 0, kSum, 0, 0};
+    if (lead && s.n > 0 && (threadIdx.x & 63) == 0) s.path[0] = 0;
+    return st;
+}
+
+// Grid (workgroups of a sequence, sequences).
+__global__ __launch_bounds__(kRoundThreads) void verify_round_kernel(const VerifyArgs a, int round)
+{
+    __shared__ State sh;
+    const int tid = threadIdx.x, b = blockIdx.y;
+    const Seq s = sequence(a, b);
+    if (s.n == 0) return;
+    const bool lead = blockIdx.x == 0;
+    if (tid < 64) {
+        State st;
+        if (round == 0) {
+            st = start(s, lead);
+            walk(a, s, st, lead);
+        } else {
+            st = a.states[(int64_t)((round - 1) & 1) * a.B + b];
+            if (st.need == kNextZ) {
+                st.Z = add_tiles(a.sums + ((int64_t)st.buf * a.B + b) * a.tiles, a.tiles);
+                st.fresh = 1;
+                walk(a, s, st, lead);
+            } else {
+                st.need = kNothing;              // the last round's pass was the last row's
+            }
+        }
+        if (st.need != kNothing) st.buf = round & 1;
+        if (tid == 0) {
+            sh = st;
+            if (lead) a.states[(int64_t)(round & 1) * a.B + b] = st;
+        }
+    }
+    __syncthreads();
+    const State st = sh;
+    if (st.need == kNothing) return;
+    tile_sums<false>(a, row_of(a, s, st), kRoundWaves * blockIdx.x + (tid >> 6), kRoundWaves * gridDim.x,
+              a.sums + ((int64_t)st.buf * a.B + b) * a.tiles);
+}
+
+// Inclusive sums of a wave's lanes.
+__device__ __forceinline__ double wave_scan(double c)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const double o = __shfl_up(c, off);
+        if (lane >= off) c += o;
+    }
+    return c;
+}
+
+// The first token whose cumulated sum passes t (all lanes of one wave): the tile, then its pieces. Where
+// rounding leaves none it is the last token with anything, as in each step of the search.
+__device__ __forceinline__ int32_t draw(const VerifyArgs &a, const Row &r, const double *sums, double t)
+{
+    const int lane = threadIdx.x & 63;
+    int32_t tile = -1, some = 0;                            // some: the last tile with anything
+    double before = 0.0;
+    for (int32_t t0 = 0; t0 < a.tiles && tile < 0; t0 += 64) {
+        const double x = t0 + lane < a.tiles ? sums[t0 + lane] : 0.0, c = wave_scan(x);
+        const uint64_t any = __builtin_amdgcn_ballot_w64(x > 0.0);
+        const uint64_t over = __builtin_amdgcn_ballot_w64(x > 0.0 && before + c > t);
+        if (any) some = t0 + 63 - (int32_t)__builtin_clzll(any);
+        if (over) {
+            const int l = (int)__builtin_ctzll(over);
+            tile = t0 + l;
+            before += __shfl(c, l) - __shfl(x, l);
+        } else {
+            before += __shfl(c, 63);
+        }
+    }
+    t = tile < 0 ? INFINITY : t - before;
+    tile = tile < 0 ? some : tile;
+    before = 0.0;
+    int32_t token = -1, last = 0;                           // the token, and the last one with anything
+    for (int32_t piece = 0; piece < a.pieces && token < 0; ++piece) {
+        const int32_t base = (int32_t)min(((int64_t)tile * a.pieces + piece) * kPiece, (int64_t)a.V);
+        Four x[kVecs];
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) x[k] = load(r, a.V, base + k * 256 + 4 * lane);
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            double e[4];
+            values(r, x[k], base + k * 256, base + k * 256 + 4 * lane, a.V, e);
+            const double y = (e[0] + e[1]) + (e[2] + e[3]), c = wave_scan(y);
+            const uint64_t any = __builtin_amdgcn_ballot_w64(y > 0.0);
+            const uint64_t over = __builtin_amdgcn_ballot_w64(y > 0.0 && before + c > t);
+            if (any && token < 0) {
+                const int l = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(any);
+                double z = before + (c - y);
+                int32_t m = -1, end = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z += e[i];
+                    if (m < 0 && e[i] > 0.0 && z > t) m = i;
+                    if (e[i] > 0.0) end = i;
+                }
+                last = base + k * 256 + 4 * l + __shfl(over && m >= 0 ? m : end, l);
+                if (over) token = last;
+            }
+            before += __shfl(c, 63);
+        }
+    }
+    return token < 0 ? last : token;
+}
+
+// One workgroup per sequence.
+__global__ __launch_bounds__(kFinalThreads) void verify_final_kernel(const VerifyArgs a)
+{
+    __shared__ State sh;
+    __shared__ double sums[kMaxTiles];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x;
+    const Seq s = sequence(a, b);
+    const float u0 = s.n > 0 ? s.uniforms[0] : 0.f;
+    State st;
+    if (wave == 0) {
+        if (a.rounds == 0 || s.n == 0) {
+            st = start(s, true);
+            walk(a, s, st, true);
+        } else {
+            st = a.states[(int64_t)((a.rounds - 1) & 1) * a.B + b];
+            // (with one round the sums are read beside the state, not behind it)
+            const double *from = a.sums + ((int64_t)(a.rounds == 1 ? 0 : st.buf) * a.B + b) * a.tiles;
+            for (int32_t t = lane; t < a.tiles; t += 64) sums[t] = from[t];
+            if (st.need == kNextZ) {
+                st.Z = add_tiles(sums, a.tiles);
+                st.fresh = 1;
+                walk(a, s, st, true);
+            } else {
+                st.need = kNothing;
+            }
+        }
+        if (lane == 0) sh = st;
+    }
+    __syncthreads();
+    st = sh;
+    while (s.n > 0 && st.need != kNothing) {
+        tile_sums<true>(a, row_of(a, s, st), wave, kFinalThreads / 64, sums);
+        __syncthreads();
+        if (wave == 0) {
+            if (st.need == kNextZ) {
+                st.Z = add_tiles(sums, a.tiles);
+                st.fresh = 1;
+                walk(a, s, st, true);
+            } else {
+                st.need = kNothing;
+            }
+            if (lane == 0) sh = st;
+        }
+        __syncthreads();
+        st = sh;
+    }
+    for (int32_t i = st.kept + tid; i < a.path_cap; i += kFinalThreads) s.path[i] = -1;
+    if (tid == 0) {
+        a.accepted_lens[b] = st.kept;
+        a.context_lens[b] = a.prefix_lens[b] + st.kept;
+        if (s.n == 0) a.next_tokens[b] = -1;
+    }
+    if (s.n == 0) return;
+    Row r = row_of(a, s, st);
+    double S = add_tiles(sums, a.tiles);
+    if (!(S > 0.0)) {                                       // nothing is left: the target's own row
+        r.q = nullptr;
+        r.a = 0.0;
+        r.end = r.at + 1;
+        __syncthreads();
+        tile_sums<true>(a, r, wave, kFinalThreads / 64, sums);
+        __syncthreads();
+        S = add_tiles(sums, a.tiles);
+    }
+    if (wave > 0) return;
+    const int32_t token = draw(a, r, sums, (double)u0 * S);
+    if (lane == 0) a.next_tokens[b] = token;
+}
+
+// How a call is cut up.
+constexpr int32_t kRoundSeqs = 1024;      // sequences up to which there are rounds
+struct Plan {
+    int32_t tiles, pieces, rounds, wgs;
+    int64_t bytes;                        // of workspace
+};
+// Rounds: none where one workgroup sums a row in a few steps (up to 8 tiles; one sequence of 32 took 12.5 us
+// without and 11.7 with a round), or where the sequences alone fill the device. One for a draft
+// without probabilities, which needs one sum, and for short drafts: a chain of 4 needs one sum too (64 of 128000
+// tokens: 30.7 us without a round, 22.3 with one, 28.6 with two, each idle one 2.8). Trees refuse more: a pass in
+// the last launch, with one workgroup per sequence, takes about 15 us of 128000 tokens, in a round
+// 5 and less (128 trees of 12: 94 us without, 106, 102, 83, 67 and 75 with one to five); of few tiles a pass
+// takes no more than an idle round.
+Plan make_plan(int32_t B, int32_t T, int32_t V, bool drawn)
+{
+    Plan p{};
+    p.pieces = (int32_t)(((int64_t)V + (int64_t)kPiece * kMaxTiles - 1) / ((int64_t)kPiece * kMaxTiles));
+    const int64_t size = (int64_t)p.pieces * kPiece;
+    p.tiles = (int32_t)((V + size - 1) / size);
+    const int64_t nodes = ((int64_t)T + std::max(B, 1) - 1) / std::max(B, 1);
+    p.rounds = p.tiles <= 8 || B > kRoundSeqs ? 0 : !drawn || nodes <= 5 || p.tiles < 48 ? 1 : nodes <= 9 ? 2 : 4;
+    p.wgs = (int32_t)std::min<int64_t>((p.tiles + kRoundWaves - 1) / kRoundWaves, std::max<int64_t>(1, 4096 / std::max(B, 1)));
+    p.bytes = p.rounds ? (int64_t)2 * B * (sizeof(State) + 8 * p.tiles) : 0;
+    return p;
 }
 
 }  // namespace
@@ -179,6 +484,7 @@ pcr_status pcr_verify_drafts_workspace_size(int32_t B, int32_t T, int32_t vocab,
     if (!bytes) return fail(PCR_ERR_INVALID_ARG, "%s: bytes is NULL", who);
     *bytes = 0;
     if (B < 0 || T < 0 || vocab < 1) return fail(PCR_ERR_INVALID_ARG, "%s: negative B or T, or vocab < 1", who);
+    if (B > 0) *bytes = make_plan(std::min(B, kRoundSeqs), T, vocab, true).bytes;
     return PCR_OK;
 }
 
@@ -203,10 +509,28 @@ pcr_status pcr_verify_drafts(int32_t B, const int32_t *cu_nodes, const int32_t *
     if (!cu_nodes || !prefix_lens || !path || !accepted_lens || !next_tokens || !context_lens ||
         (T > 0 && (!parents || !tokens || !target_probs || !uniforms)))
         return fail(PCR_ERR_INVALID_ARG, "%s: NULL argument", who);
+    const Plan plan = make_plan(B, T, vocab, draft_probs != nullptr);
+    if (plan.bytes > 0) {
+        if (!workspace || workspace_bytes < plan.bytes)
+            return fail(PCR_ERR_INVALID_ARG, "%s: this batch needs a workspace of %lld bytes (%lld given)", who,
+                        (long long)plan.bytes, (long long)(workspace ? workspace_bytes : 0));
+        if ((uintptr_t)workspace & 15)
+            return fail(PCR_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+    }
+    State *states = static_cast<State *>(workspace);
     const VerifyArgs a{cu_nodes, parents, tokens, prefix_lens, target_probs, draft_probs, uniforms, target_stride,
-                       draft_stride, path, accepted_lens, next_tokens, context_lens, T, vocab, path_cap};
-    hipLaunchKernelGGL(verify_kernel, dim3(B), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
-    const hipError_t e = hipGetLastError();
+                       draft_stride, path, accepted_lens, next_tokens, context_lens, B, T, vocab, path_cap, plan.tiles,
+                       plan.pieces, plan.rounds, states, reinterpret_cast<double *>(states + 2 * (int64_t)B)};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = hipSuccess;
+    for (int r = 0; r < plan.rounds && e == hipSuccess; ++r) {
+        hipLaunchKernelGGL(verify_round_kernel, dim3(plan.wgs, B), dim3(kRoundThreads), 0, s, a, r);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) {
+        hipLaunchKernelGGL(verify_final_kernel, dim3(B), dim3(kFinalThreads), 0, s, a);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess) return hip_fail(e, "pcr_verify_drafts: launch");
     return PCR_OK;
 }
