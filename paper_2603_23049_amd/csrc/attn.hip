@@ -26,6 +26,12 @@
 // decode workgroup (all its columns see the same keys), and a key split leaves its partial
 // results in the caller's workspace. Sequences without keys are not part of the launch.
 //
+// A tree of drafted tokens (TREE; tree.hip) has the causal form's keys, p cached ones and s new ones, of which
+// a row sees the cached ones and those that its bits name. A row sees none of a tile, of its
+// keys' half or at all as easily as it sees some; and since the slot of a node that it does not see may
+// hold anything, V entries of nodes that are infinite or NaN are cleared in LDS by the wave that
+// loaded them, before the tile's product (0 * inf is NaN), and given at the end to the rows that see them.
+//
 // Per wave and 64-key tile (4 pool blocks), with v_mfma_f32_32x32x16_bf16:
 //   S^T[key][q] = K Q^T   A = K rows from LDS, B = this wave's Q (registers)
 //   O^T[d][q]  += V^T P^T A = V^T from LDS,  B = P (registers)
@@ -195,7 +201,9 @@ struct AttnWorkMap {
     int32_t per_head;                   // work items of all sequences, one kv head
     int32_t chunk;                      // key split: 64-key tiles per item (else unused)
     uint64_t launch;                    // key split: the launch's number (else unused)
-    char *workspace;                    // key split of cross attention: its partial results
+    char *workspace;                    // key split of cross and tree attention: its partial results
+    const uint64_t *visible;            // tree attention: the rows' words, and how many a row has
+    int32_t words;
     int32_t seq[kMaxMapSeqs];           // sequence in each slot
     int32_t tiles_end[kMaxMapSeqs];     // items of the slots up to and including this one
     int32_t prefix[kMaxMapSeqs];        // the slot's cached tokens p (cross attention: its keys n)
@@ -240,17 +248,20 @@ __device__ SplitControl split_control;
 __device__ __attribute__((aligned(1024))) char split_o[kSplitSlots][kSplitParts][kSplitPartO];
 __device__ __attribute__((aligned(1024))) char split_ml[kSplitSlots][kSplitParts][kSplitPartML];
 
-// Partial results of part 0: in the library's scratch, or in the workspace of a cross attention
+// Which keys a row sees (see the head of this file).
+enum AttnKind { kCausal = 0, kCross = 1, kTree = 2 };
+
+// Partial results of part 0: in the library's scratch, or in the workspace of a cross or tree attention
 // call (parts' O, then their maxima and sums).
-template <bool CROSS>
+template <int KIND>
 __device__ __forceinline__ char *split_part_o(const AttnWorkMap &wm)
 {
-    return CROSS ? wm.workspace : &split_o[0][0][0];
+    return KIND != kCausal ? wm.workspace : &split_o[0][0][0];
 }
-template <bool CROSS>
+template <int KIND>
 __device__ __forceinline__ char *split_part_ml(const AttnWorkMap &wm)
 {
-    return CROSS ? wm.workspace + (int64_t)kSplitParts * kSplitPartO : &split_ml[0][0][0];
+    return KIND != kCausal ? wm.workspace + (int64_t)kSplitParts * kSplitPartO : &split_ml[0][0][0];
 }
 
 // The entry owned by the launch with this number (wave-uniform), or -1. From kSplitSlots on
@@ -443,13 +454,24 @@ __device__ __forceinline__ void store_rows(const char *stage, int lane, int orow
 }
 
 // A sequence whose rows one decode workgroup takes.
-template <bool CROSS>
+template <int KIND>
 __device__ __host__ __forceinline__ bool few_rows(int s, int G)
 {
-    return CROSS ? s * G <= decode_wave::kMaxCols : s == 1 && G <= decode_wave::kMaxCols;
+    return KIND == kCross ? s * G <= decode_wave::kMaxCols
+                          : KIND == kCausal && s == 1 && G <= decode_wave::kMaxCols;
 }
 
-template <int D, int MODE, bool CROSS>
+// Bits [d, d + 64) of a row's words, where bits below 0 are set and those from n on are not.
+__device__ __forceinline__ uint64_t seen64(const uint64_t *__restrict__ words, int n_words, int d, int n)
+{
+    const int lo = max(d, 0), w = lo >> 6, sh = lo & 63;
+    uint64_t x = w < n_words ? words[w] >> sh : 0ull;
+    if (sh > 0 && w + 1 < n_words) x |= words[w + 1] << (64 - sh);
+    if (d < 0) x = (x << -d) | ((1ull << -d) - 1);          // (d > -64: a tile with nodes)
+    return d + 64 > n ? x & (n > d ? (1ull << (n - d)) - 1 : 0ull) : x;
+}
+
+template <int D, int MODE, int KIND>
 __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const u16 *__restrict__ q, const u16 *__restrict__ pool_k, const u16 *__restrict__ pool_v,
     int32_t num_blocks, int32_t Hkv, const int32_t *__restrict__ block_tables, int32_t max_blocks, int32_t Hq,
@@ -464,12 +486,14 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     static_assert(kGroupWaves % kSlabs == 0, "slab-to-wave mapping");
     constexpr int kKLoads = Geo::KLOADS, kVLoads = Geo::VLOADS;
     constexpr bool ROWS = MODE == kRowHalves;
+    constexpr bool CROSS = KIND == kCross, TREE = KIND == kTree;
     constexpr int RPW = ROWS ? 2 * kRowsPerWG : kRowsPerWG;   // packed rows per workgroup
 
     // Per group: K buffers 0/1 then V buffers 0/1 (double-buffered, tile j in buffer j&1);
     // with row halves both groups use group 0's. The whole array is reused for the merge
     // at the end of key halves.
     __shared__ __attribute__((aligned(1024))) char lds[2][2 * (Geo::KBYTES + Geo::VBYTES)];
+    __shared__ int odd_nodes;      // TREE: a node's V holds an infinity or NaN
 
     const int tid = threadIdx.x, lane = tid & 63;
     const Item it = locate_item(wm, Hkv);
@@ -482,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         const int ns = (key_tiles(CROSS ? p - 1 : p + s - 1) + wm.chunk - 1) / wm.chunk;
         rt = it.local / ns;
         sp = it.local - rt * ns;
-        const int slot = CROSS ? 0 : split_entry(wm.launch);
+        const int slot = KIND != kCausal ? 0 : split_entry(wm.launch);
         const bool whole = slot < 0 || slot >= kSplitSlots;
         if (whole && sp > 0) return;                 // unsplit: chunk 0 takes every key
         if (!whole) part = slot * kSplitParts + g * wm.per_head + it.j;
@@ -496,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const int rows_total = s * G;
     const int row0 = rt * RPW;
     if (s <= 0 || row0 >= rows_total || T <= 0) return;   // uniform over the workgroup
-    if (few_rows<CROSS>(s, G)) {                          // a decode row (uniform too)
+    if (few_rows<KIND>(s, G)) {                           // a decode row (uniform too)
         static_assert(kThreads / 64 * (D / 16) * 64 * 16 + kThreads / 64 * 64 * 8 <= (int)sizeof(lds), "merge area");
         if (t0 >= T) return;
         int n0 = 0, n_keys = CROSS ? p : p + 1;      // keys 0 .. p: the row's causal range
@@ -506,8 +530,8 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
             if (part >= 0 && n_keys > wm.chunk * kTileKeys) {
                 n0 = sp * wm.chunk * kTileKeys;
                 n_keys = min(n_keys, n0 + wm.chunk * kTileKeys);
-                po = reinterpret_cast<f32x4 *>(split_part_o<CROSS>(wm) + (int64_t)part * kSplitPartO);
-                pml = reinterpret_cast<float *>(split_part_ml<CROSS>(wm) + (int64_t)part * kSplitPartML);
+                po = reinterpret_cast<f32x4 *>(split_part_o<KIND>(wm) + (int64_t)part * kSplitPartO);
+                pml = reinterpret_cast<float *>(split_part_ml<KIND>(wm) + (int64_t)part * kSplitPartML);
             }
         }
         decode_workgroup<D, CROSS>(q, pool_k, pool_v, num_blocks, Hkv, block_tables + (int64_t)b * max_blocks,
@@ -530,7 +554,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     asm volatile("" : "+v"(orow));
 
     const int wg_last = min(rows_total - 1, row0 + RPW - 1);
-    const int all_tiles = key_tiles(CROSS ? p - 1 : p + wg_last / G);
+    const int all_tiles = key_tiles(CROSS ? p - 1 : TREE ? p + s - 1 : p + wg_last / G);
     // This workgroup's tiles [t_lo, t_lo + ntiles): all, or a chunk of a key split.
     int t_lo = 0, ntiles = all_tiles;
     if constexpr (MODE == kKeySplit) {
@@ -547,7 +571,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const int tile_begin = t_lo + ((!ROWS && grp) ? split : 0);
     const int n = (ROWS || !grp) ? split : ntiles - split;        // this group's tiles
     const int w_first = min(rows_total - 1, wrow0);
-    const int w_min_limit = CROSS ? p - 1 : p + w_first / G;
+    const int w_min_limit = CROSS || TREE ? p - 1 : p + w_first / G;
     const int valid_blocks = min((total + kBlockSize - 1) / kBlockSize, max_blocks);
 
     bf16x8 qf[KSTEPS];    // the Q^T operand (k-step ks: dims 16ks + 8half .. +7 of this lane's row)
@@ -764,11 +788,22 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         __builtin_amdgcn_s_setprio(0);
     };
 
+    // TREE: this lane's row's words (from the row of the output, which the loop holds anyway).
+    auto row_words = [&]() __attribute__((always_inline)) { return wm.visible + (int64_t)(max(orow, 0) / Hq) * wm.words; };
     // ---- vector work: online softmax of S^T(j) into bf16 P(j) (lazy rescale) ----
     auto softmax = [&](int j, f32x16 (&st)[2], bf16x8 (&pf)[kTileBlocks]) __attribute__((always_inline)) {
         l_run += (lane & 16) ? tsum[1] : tsum[0];   // tile j-1 (zero before the first tile)
         const int kbase = (tile_begin + j) * kTileKeys;
-        if (kbase + kTileKeys - 1 > w_min_limit) {
+        if (TREE && kbase + kTileKeys - 1 > w_min_limit) {
+            const uint64_t seen = seen64(row_words(), wm.words, kbase - p, s) >> (8 * half);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const uint32_t bits = (uint32_t)(seen >> (32 * m));
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    st[m][r] = (bits >> (16 * (r >> 3) + (r & 7))) & 1u ? st[m][r] : -INFINITY;
+            }
+        } else if (!TREE && kbase + kTileKeys - 1 > w_min_limit) {
             // register r of half tile m holds key kbase + 32m + 16(r/8) + 8half + r%8
             const int lim = limit - kbase - 8 * half;
 #pragma unroll
@@ -798,6 +833,19 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
             const auto sw = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
             const unsigned lo = sw[0], hi = sw[1];
             mx = __builtin_elementwise_maximum(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
+        }
+        if constexpr (TREE) {
+            // A row with a score that is infinite or NaN is NaN: its sum becomes that here and its P 0, since the
+            // row sums' product, which two rows share, would carry a NaN from one to the other.
+            const bool lost = !(mx < INFINITY);
+            if (__builtin_amdgcn_ballot_w64(lost)) {
+                l_run = lost ? __builtin_nanf("") : l_run;
+                mx = lost ? -INFINITY : mx;
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) st[m][r] = lost ? -INFINITY : st[m][r];
+            }
         }
         const bool need = mx > thr;
         if (__builtin_amdgcn_ballot_w64(need)) {
@@ -854,6 +902,7 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
     const bool loader = !ROWS || grp == 0;
     int64_t ids_v[kTileBlocks], ids_k[kTileBlocks];   // payload byte offsets
     int32_t ids_next[kTileBlocks];
+    if (TREE && tid == 0) odd_nodes = 0;
     tile_ids(0, ids_raw);
     tile_ids(1, ids_next);
     to_offs(ids_raw, ids_v);
@@ -900,6 +949,31 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         phase_barrier();
         ++ph;
     };
+    // TREE: of the V(j) chunks that this wave loaded (each lane its own 16 bytes), the infinite and NaN
+    // entries of nodes and whatever lies past the last one are cleared.
+    auto clean_v = [&](int j) __attribute__((always_inline)) {
+        const int chunk = (wg % kSlabs) * 64 + lane, d = chunk >> 1, pch = (chunk & 1) ^ ((d >> 3) & 1);
+        uint32_t odd = 0;
+#pragma unroll 1
+        for (int u = 0; u < kVLoads; ++u) {
+            const int slab = u * kGroupWaves + wg;
+            const int k0 = (tile_begin + j) * kTileKeys + 16 * (slab / kSlabs) + 8 * pch;    // the chunk's 8 keys
+            u32x4 *at = reinterpret_cast<u32x4 *>(vbuf(j) + slab * 1024 + lane * 16);
+            u32x4 v = *at;
+            uint32_t any = 0;
+#pragma unroll
+            for (int wd = 0; wd < 4; ++wd) {
+                const int k = k0 + 2 * wd;
+                const uint32_t bad = ((v[wd] & 0x7F80u) == 0x7F80u && k >= p ? 0xFFFFu : 0u) |
+                                     ((v[wd] & 0x7F800000u) == 0x7F800000u && k + 1 >= p ? 0xFFFF0000u : 0u);
+                odd |= bad & ((k < total ? 0xFFFFu : 0u) | (k + 1 < total ? 0xFFFF0000u : 0u));
+                any |= bad;
+                v[wd] &= ~bad;
+            }
+            if (any) *at = v;
+        }
+        if (odd) odd_nodes = 1;
+    };
     // M(j): softmax of tile j; block ids of tile j+2 (read now, range-checked and
     // converted at the start of C(j)) when this group loads; then wait for the loads
     // C(j-1) issued.
@@ -910,6 +984,9 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         __builtin_amdgcn_sched_barrier(0);
         softmax(j, st, pf);
         wait_vmem();
+        if constexpr (TREE && decltype(load_tag)::value) {
+            if ((tile_begin + j + 1) * kTileKeys > p) clean_v(j);
+        }
         // The id loads landed long ago; an explicit wait here (seen by the compiler) keeps
         // it from placing one among the next matrix cluster's fragment reads.
         __builtin_amdgcn_sched_barrier(0);
@@ -960,8 +1037,8 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         }
         vector_cluster(n - 1, st, pf, load_tag);
         phase_end();
-        // The group's last tile may hold the sequence end: clear V past it.
-        if ((tile_begin + n) * kTileKeys > total) pv(n - 1, pf, T_);
+        // The group's last tile may hold the sequence end: clear V past it (TREE: done where it was loaded).
+        if (!TREE && (tile_begin + n) * kTileKeys > total) pv(n - 1, pf, T_);
         else matrix_cluster(T_, F_, n - 1, pf, st, ids_v, ids_k, F_, load_tag);
         phase_end();
     };
@@ -970,11 +1047,30 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         else run_tiles(std::false_type{});
     }
     while (ph < phases) phase_end();
+    if constexpr (TREE) {
+        // Infinite and NaN entries of the nodes that this lane's row sees, which the products took as 0.
+        if (odd_nodes) {
+            const uint64_t *words = row_words();
+            const int last = min(total, (tile_begin + n) * kTileKeys);
+            for (int k = max(p, tile_begin * kTileKeys); k < last; ++k) {
+                const bool sees = (words[(k - p) >> 6] >> ((k - p) & 63)) & 1;
+                const u16 *v = reinterpret_cast<const u16 *>(pool_v_bytes + payload_off(bt[k / kBlockSize])) + k % kBlockSize;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t x = v[(32 * mt + 8 * (r >> 2) + 4 * half + (r & 3)) * kBlockSize];
+                        if (sees && (x & 0x7F80u) == 0x7F80u) o_acc[mt][r] += __builtin_bit_cast(float, x << 16);
+                    }
+            }
+        }
+    }
 
     if constexpr (ROWS) {
         // ---- row halves: every group saw all keys of its rows; normalise, store ----
         // (the last phase's barrier is behind every read of the tile buffers)
-        const float inv = 1.f / (l_run + ((lane & 16) ? tsum[1] : tsum[0]));
+        const float l_all = l_run + ((lane & 16) ? tsum[1] : tsum[0]);
+        const float inv = TREE && l_all == 0.f ? 0.f : 1.f / l_all;    // (a row that sees nothing is zeros)
         char *stage = &lds[0][0] + wave * (32 * D * 2);
 #pragma unroll
         for (int k = 0; k < MT; ++k)
@@ -1027,9 +1123,9 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
         if (part >= 0) {
             // A chunk's partial result, in the lane layout (1 KB per wave-wide store).
             if (orow >= 0) {
-                f32x4 *po = reinterpret_cast<f32x4 *>(split_part_o<CROSS>(wm) + (int64_t)part * kSplitPartO) +
+                f32x4 *po = reinterpret_cast<f32x4 *>(split_part_o<KIND>(wm) + (int64_t)part * kSplitPartO) +
                             wg * MT * 4 * 64 + lane;
-                f32x2 *pml = reinterpret_cast<f32x2 *>(split_part_ml<CROSS>(wm) + (int64_t)part * kSplitPartML) +
+                f32x2 *pml = reinterpret_cast<f32x2 *>(split_part_ml<KIND>(wm) + (int64_t)part * kSplitPartML) +
                              wg * 64 + lane;
 #pragma unroll
                 for (int k = 0; k < MH; ++k)
@@ -1046,7 +1142,8 @@ __global__ __launch_bounds__(kThreads) void prefill_attn_kernel(
             return;
         }
     }
-    const float inv = 1.f / (a0 * l_tot + a1 * l1);
+    const float l_all = a0 * l_tot + a1 * l1;
+    const float inv = TREE && l_all == 0.f ? 0.f : 1.f / l_all;
     char *stage = &lds[0][0] + 2 * kGroupWaves * XW * 64 * 16 + wave * (32 * MH * 32 * 2);
     static_assert(2 * kGroupWaves * (XW * 64 * 16 + 32 * MH * 32 * 2) <= (int)sizeof(lds), "merge and output area");
 #pragma unroll
@@ -1158,14 +1255,15 @@ __global__ __launch_bounds__(64) void split_release_kernel(uint64_t launch, unsi
 // dims) are dealt to the waves of all its chunks' workgroups, so the reads of the
 // partial results, which bound this kernel, come from every compute unit.
 constexpr int kCombineThreads = 512;
-template <int D, bool CROSS>
+template <int D, int KIND>
 __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t Hkv, int32_t Hq, int32_t T,
                                                                         float scale_log2, u16 *__restrict__ out,
                                                                         const AttnWorkMap wm)
 {
     constexpr int MT = D / 32;
     constexpr int kCombineWaves = kCombineThreads / 64;
-    const int slot = CROSS ? 0 : split_entry(wm.launch);
+    constexpr bool CROSS = KIND == kCross, TREE = KIND == kTree;
+    const int slot = KIND != kCausal ? 0 : split_entry(wm.launch);
     if (slot < 0) return;                            // ran unsplit
     const Item it = locate_item(wm, Hkv);
     const int lane = threadIdx.x & 63;
@@ -1176,14 +1274,14 @@ __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t 
         const int ns_seq = (key_tiles(CROSS ? p - 1 : p + s - 1) + wm.chunk - 1) / wm.chunk;
         const int rt = it.local / ns_seq, sp = it.local - rt * ns_seq;
         const int row0 = rt * kRowsPerWG;
-        const bool decode_row = few_rows<CROSS>(s, G);
+        const bool decode_row = few_rows<KIND>(s, G);
         const int wg_last = min(rows_total - 1, row0 + kRowsPerWG - 1);
         const int ns =                                        // chunks of this row tile
-            (key_tiles(CROSS ? p - 1 : p + wg_last / G) + wm.chunk - 1) / wm.chunk;
+            (key_tiles(CROSS ? p - 1 : TREE ? p + s - 1 : p + wg_last / G) + wm.chunk - 1) / wm.chunk;
         // chunk s of the row tile is item j + sp - s (items count down)
         const int64_t part0 = (int64_t)slot * kSplitParts + it.g * wm.per_head + it.j + sp;
-        const f32x4 *po = reinterpret_cast<const f32x4 *>(split_part_o<CROSS>(wm));
-        const f32x2 *pml = reinterpret_cast<const f32x2 *>(split_part_ml<CROSS>(wm));
+        const f32x4 *po = reinterpret_cast<const f32x4 *>(split_part_o<KIND>(wm));
+        const f32x2 *pml = reinterpret_cast<const f32x2 *>(split_part_ml<KIND>(wm));
         const int waves = (wg_last - row0) / kRowsPerWave + 1;   // of the row tile, with rows
         const int pieces = ns <= 1 || row0 >= rows_total ? 0 : decode_row ? D / 16 : waves * MT * 4;
         const float c = decode_row ? 1.f : scale_log2;    // a decode row's max is scaled already
@@ -1242,11 +1340,11 @@ __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t 
             };
             if (ns <= 4) merge(std::integral_constant<int, 4>{});
             else merge(std::integral_constant<int, 16>{});
-            const bf16x4 bv = __builtin_convertvector(acc * (1.f / L), bf16x4);
+            const bf16x4 bv = __builtin_convertvector(acc * (TREE && L == 0.f ? 0.f : 1.f / L), bf16x4);
             *reinterpret_cast<u32x2 *>(out + (tq * Hq + h) * D + d0) = __builtin_bit_cast(u32x2, bv);
         }
     }
-    if constexpr (CROSS) return;                     // (the workspace is the caller's)
+    if constexpr (KIND != kCausal) return;           // (the workspace is the caller's)
     // This workgroup is through with the slot: it only reads it, and every read has returned
     // its value before the barrier.
     __syncthreads();
@@ -1282,22 +1380,28 @@ hipError_t enqueue(void (*kernel)(P...), dim3 grid, int threads, hipStream_t s, 
 
 // A launch's sequences: which keys their rows see.
 struct Seqs {
-    const int32_t *keys;      // cached tokens p (causal), or all keys n (cross attention)
+    const int32_t *keys;      // cached tokens p (causal, tree), or all keys n (cross attention)
     const int32_t *cu;        // rows
-    bool cross;
+    AttnKind kind;
     int G;
     int32_t rows(int32_t b) const { return cu[b + 1] - cu[b]; }
     // last key of row i of sequence b
-    int32_t last(int32_t b, int32_t i) const { return cross ? keys[b] - 1 : keys[b] + i; }
-    bool few(int32_t b) const { return cross ? few_rows<true>(rows(b), G) : few_rows<false>(rows(b), G); }
+    int32_t last(int32_t b, int32_t i) const
+    {
+        return kind == kCross ? keys[b] - 1 : kind == kTree ? keys[b] + rows(b) - 1 : keys[b] + i;
+    }
+    bool few(int32_t b) const
+    {
+        return kind == kCross ? few_rows<kCross>(rows(b), G) : kind == kCausal && few_rows<kCausal>(rows(b), G);
+    }
 };
 
-template <int D, int MODE, bool CROSS>
+template <int D, int MODE, int KIND>
 void launch_attn(dim3 grid, hipStream_t s, const u16 *qq, const u16 *pk, const u16 *pv, const pcr_kv_pool &pool,
                  const int32_t *block_tables, int32_t max_blocks, int32_t num_q_heads, int32_t T, float scale_log2,
                  float rescale_thr, u16 *oo, const AttnWorkMap &wm)
 {
-    hipLaunchKernelGGL((prefill_attn_kernel<D, MODE, CROSS>), grid, dim3(kThreads), 0, s, qq, pk, pv, pool.num_blocks,
+    hipLaunchKernelGGL((prefill_attn_kernel<D, MODE, KIND>), grid, dim3(kThreads), 0, s, qq, pk, pv, pool.num_blocks,
                        pool.num_kv_heads, block_tables, max_blocks, num_q_heads, T, scale_log2, rescale_thr, oo,
                        wm);
 }
@@ -1436,16 +1540,16 @@ double schedule_time(const int32_t *order, int n, const Seqs &q, int Hkv, int D,
 
 // One launch over the sequences seq[0..n) (each with new tokens, n <= kMaxMapSeqs,
 // longest context first): builds the work map, picks the schedule, launches. split_ws: of
-// cross attention, the workspace of a key split.
-template <bool CROSS>
+// cross and tree attention, the workspace of a key split; visible, words: of tree attention.
+template <int KIND>
 hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_pool &pool,
                         const int32_t *block_tables, int32_t max_blocks, const int32_t *host_prefix_lens,
                         const int32_t *host_cu_suffix, int32_t num_q_heads, int32_t T, float scale_log2,
                         float rescale_thr, u16 *oo, hipStream_t s, int auto_schedule, int n_cu, bool can_split,
-                        void *split_ws)
+                        void *split_ws, const uint64_t *visible, int32_t words)
 {
     const int Hkv = pool.num_kv_heads, G = num_q_heads / Hkv;
-    const Seqs sq{host_prefix_lens, host_cu_suffix, CROSS, G};
+    const Seqs sq{host_prefix_lens, host_cu_suffix, (AttnKind)KIND, G};
     auto rows_of = [&](int32_t b) { return (int64_t)sq.rows(b) * G; };
     const int sched = g_schedule.load(std::memory_order_relaxed);
     const bool prefer_keys = auto_schedule == PCR_ATTN_SCHEDULE_KEY_HALVES;
@@ -1530,8 +1634,10 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     wm.n_seq = n;
     wm.per_head = cum;
     wm.chunk = chunk;
-    wm.launch = chunk && !CROSS ? next_launch() : 0;
+    wm.launch = chunk && KIND == kCausal ? next_launch() : 0;
     wm.workspace = static_cast<char *>(split_ws);
+    wm.visible = visible;
+    wm.words = words;
     const int64_t n_items = (Hkv % kXcds == 0) ? (int64_t)cum * Hkv : ((int64_t)cum * Hkv + kXcds - 1) / kXcds * kXcds;
     const dim3 grid((unsigned)n_items);
     auto *pk = static_cast<const u16 *>(pool.k);
@@ -1539,18 +1645,18 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     auto launch = [&](auto dim) -> hipError_t {
         constexpr int D = decltype(dim)::value;
         auto attn = [&](auto mode) {
-            launch_attn<D, decltype(mode)::value, CROSS>(grid, s, qq, pk, pv, pool, block_tables, max_blocks, num_q_heads,
+            launch_attn<D, decltype(mode)::value, KIND>(grid, s, qq, pk, pv, pool, block_tables, max_blocks, num_q_heads,
                                                          T, scale_log2, rescale_thr, oo, wm);
         };
         if (rows) {
             attn(std::integral_constant<int, kRowHalves>{});
         } else if (!chunk) {
             attn(std::integral_constant<int, kKeyHalves>{});
-        } else if constexpr (CROSS) {
-            hipError_t e = enqueue(prefill_attn_kernel<D, kKeySplit, true>, grid, kThreads, s, qq, pk, pv, pool.num_blocks,
+        } else if constexpr (KIND != kCausal) {
+            hipError_t e = enqueue(prefill_attn_kernel<D, kKeySplit, KIND>, grid, kThreads, s, qq, pk, pv, pool.num_blocks,
                                    Hkv, block_tables, max_blocks, num_q_heads, T, scale_log2, rescale_thr, oo, wm);
             if (e == hipSuccess)
-                e = enqueue(split_combine_kernel<D, true>, grid, kCombineThreads, s, Hkv, num_q_heads, T, scale_log2,
+                e = enqueue(split_combine_kernel<D, KIND>, grid, kCombineThreads, s, Hkv, num_q_heads, T, scale_log2,
                             oo, wm);
             return e;
         } else {
@@ -1563,10 +1669,10 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
             e = enqueue(capture == hipStreamCaptureStatusNone ? split_claim_kernel : split_claim_replay_kernel,
                         dim3(1), 64, s, wm.launch, per_xcd);
             if (e != hipSuccess) return e;
-            e = enqueue(prefill_attn_kernel<D, kKeySplit, false>, grid, kThreads, s, qq, pk, pv, pool.num_blocks, Hkv,
+            e = enqueue(prefill_attn_kernel<D, kKeySplit, kCausal>, grid, kThreads, s, qq, pk, pv, pool.num_blocks, Hkv,
                         block_tables, max_blocks, num_q_heads, T, scale_log2, rescale_thr, oo, wm);
             if (e == hipSuccess)
-                e = enqueue(split_combine_kernel<D, false>, grid, kCombineThreads, s, Hkv, num_q_heads, T, scale_log2, oo,
+                e = enqueue(split_combine_kernel<D, kCausal>, grid, kCombineThreads, s, Hkv, num_q_heads, T, scale_log2, oo,
                             wm);
             if (e != hipSuccess) {
                 (void)enqueue(split_release_kernel, dim3(1), 64, s, wm.launch, per_xcd);
@@ -1623,18 +1729,18 @@ hipError_t attn_hold_scratch(int n, int *free_entries)
 
 namespace {
 // The sequences with rows, longest context first, in as many launches as the work map takes.
-template <bool CROSS>
+template <int KIND>
 hipError_t launch_batch(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
                         const int32_t *keys, const int32_t *cu, int32_t B, int32_t num_q_heads, int32_t T,
                         float sm_scale, void *out, hipStream_t s, int auto_schedule, int n_cu, bool can_split,
-                        void *split_ws)
+                        void *split_ws, const uint64_t *visible = nullptr, int32_t words = 0)
 {
     std::vector<int32_t> seq;
     seq.reserve((size_t)std::max(B, 0));
     for (int32_t b = 0; b < B; ++b)
-        if (cu[b + 1] > cu[b] && (!CROSS || keys[b] > 0)) seq.push_back(b);
+        if (cu[b + 1] > cu[b] && (KIND != kCross || keys[b] > 0)) seq.push_back(b);
     if (seq.empty()) return hipSuccess;
-    auto context = [&](int32_t b) { return CROSS ? (int64_t)keys[b] : (int64_t)keys[b] + cu[b + 1] - cu[b]; };
+    auto context = [&](int32_t b) { return KIND == kCross ? (int64_t)keys[b] : (int64_t)keys[b] + cu[b + 1] - cu[b]; };
     std::stable_sort(seq.begin(), seq.end(), [&](int32_t a, int32_t c) { return context(a) > context(c); });
     const float scale_log2 = sm_scale * kLog2e;
     const float rescale_thr = kRescaleThreshold / scale_log2;   // in units of <q,k>
@@ -1650,8 +1756,8 @@ hipError_t launch_batch(const void *q, const pcr_kv_pool &pool, const int32_t *b
         int n = 0;
         for (int k = l; k < n_act; k += n_launch) group[n++] = seq[k];
         const hipError_t e =
-            launch_group<CROSS>(group, n, qq, pool, block_tables, max_blocks, keys, cu, num_q_heads, T, scale_log2,
-                                rescale_thr, oo, s, auto_schedule, n_cu, can_split && n_launch == 1, split_ws);
+            launch_group<KIND>(group, n, qq, pool, block_tables, max_blocks, keys, cu, num_q_heads, T, scale_log2,
+                                rescale_thr, oo, s, auto_schedule, n_cu, can_split && n_launch == 1, split_ws, visible, words);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -1668,7 +1774,7 @@ hipError_t launch_prefix_prefill_attn(const void *q, const pcr_kv_pool &pool,
     // that need no merge are written beside them: not for outputs that overlap q.
     const uintptr_t qa = (uintptr_t)q, oa = (uintptr_t)out;
     const uintptr_t bytes = (uintptr_t)T * num_q_heads * pool.head_dim * 2;
-    return launch_batch<false>(q, pool, block_tables, max_blocks, host_prefix_lens, host_cu_suffix, B, num_q_heads, T,
+    return launch_batch<kCausal>(q, pool, block_tables, max_blocks, host_prefix_lens, host_cu_suffix, B, num_q_heads, T,
                                sm_scale, out, s, auto_schedule, n_cu, qa + bytes <= oa || oa + bytes <= qa, nullptr);
 }
 
@@ -1679,8 +1785,22 @@ hipError_t launch_cross_tiles(const void *q, const pcr_kv_pool &pool, const int3
                               int32_t T, float sm_scale, void *out, void *workspace, hipStream_t s, int n_cu)
 {
     try {
-        return launch_batch<true>(q, pool, block_tables, max_blocks, host_key_lens, host_cu_q, B, num_q_heads, T,
+        return launch_batch<kCross>(q, pool, block_tables, max_blocks, host_key_lens, host_cu_q, B, num_q_heads, T,
                                   sm_scale, out, s, PCR_ATTN_SCHEDULE_AUTO, n_cu, workspace != nullptr, workspace);
+    } catch (const std::bad_alloc &) {       // (the list of sequences)
+        return hipErrorOutOfMemory;
+    }
+}
+
+hipError_t launch_tree_tiles(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
+                             const int32_t *host_prefix_lens, const int32_t *host_cu_nodes, int32_t B,
+                             const uint64_t *visible, int32_t mask_words, int32_t num_q_heads, int32_t T,
+                             float sm_scale, void *out, void *workspace, hipStream_t s, int n_cu)
+{
+    try {
+        return launch_batch<kTree>(q, pool, block_tables, max_blocks, host_prefix_lens, host_cu_nodes, B, num_q_heads, T,
+                                   sm_scale, out, s, PCR_ATTN_SCHEDULE_AUTO, n_cu, workspace != nullptr, workspace,
+                                   visible, mask_words);
     } catch (const std::bad_alloc &) {       // (the list of sequences)
         return hipErrorOutOfMemory;
     }

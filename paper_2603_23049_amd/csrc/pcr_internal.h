@@ -59,6 +59,11 @@ int64_t cross_tiles_workspace_bytes();
 hipError_t launch_cross_tiles(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
                               const int32_t *host_key_lens, const int32_t *host_cu_q, int32_t B, int32_t num_q_heads,
                               int32_t T, float sm_scale, void *out, void *workspace, hipStream_t s, int n_cu);
+// Tree attention by row tiles (attn.hip), of any number of rows; workspace as for cross attention.
+hipError_t launch_tree_tiles(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
+                             const int32_t *host_prefix_lens, const int32_t *host_cu_nodes, int32_t B,
+                             const uint64_t *visible, int32_t mask_words, int32_t num_q_heads, int32_t T,
+                             float sm_scale, void *out, void *workspace, hipStream_t s, int n_cu);
 // Compute units of the current device (queried once per device).
 pcr_status device_cu_count(int32_t *n_cu, const char *who);
 
@@ -97,6 +102,13 @@ struct CrossRowsPlan {
 };
 // pairs: of all sequences (those without steps too); longest: steps of one pair, at most.
 CrossRowsPlan cross_rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu);
+// The same with the estimate's constants: us of a compute unit for a step, what parts take with nothing to
+// read, and how much longer than other cuts even runs take to read.
+struct RowsCost {
+    float cu, parts, even;
+};
+CrossRowsPlan rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu,
+                        const RowsCost &cost);
 // Most slots of any plan (none has more than its steps, either).
 int64_t cross_rows_max_slots(int32_t head_dim, int32_t n_cu);
 // The run of an even cut that holds step x.
@@ -112,6 +124,13 @@ hipError_t launch_cross_rows(const void *q, const pcr_kv_pool &pool, const int32
                              const int32_t *key_lens, const int32_t *cu_q, int32_t B, int32_t num_q_heads, int32_t T,
                              int32_t cols, int64_t steps, const CrossRowsPlan &plan, bool combine, float sm_scale,
                              void *out, void *workspace, hipStream_t s);
+// The same of trees (tree_rows.hip): keys are the cached tokens and then the nodes, cols up to kTreeMaxCols.
+constexpr int kTreeMaxCols = 32;
+hipError_t launch_tree_rows(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
+                            const int32_t *prefix_lens, const int32_t *cu_nodes, int32_t B, const uint64_t *visible,
+                            int32_t mask_words, int32_t num_q_heads, int32_t T, int32_t cols, int64_t steps,
+                            const CrossRowsPlan &plan, bool combine, float sm_scale, void *out, void *workspace,
+                            hipStream_t s);
 // Trees of drafted tokens (draft.hip, verify.hip, tree.hip).
 constexpr int32_t kMaxMaskWords = 16;        // 64-bit words of a node's visible set
 constexpr int32_t kMaxTreeSeqs = 1 << 21;    // a workgroup of up to 1024 threads each: below 2^32 threads

@@ -3,113 +3,33 @@
 // ancestors, as pcr_draft_tree leaves them), K/V read through the block table.
 //
 // The rows of one (sequence, kv head) share its keys, so they are packed (row r = node r / G,
-// head-in-group r % G) and taken in groups of up to 32, the columns of a wave's matrix tiles
-// (tree_wave.h): K and V go from memory into registers once for all of them. A workgroup takes
-// one group; its waves share out the keys and merge in LDS.
+// head-in-group r % G). Batches whose sequences have up to 32 packed rows each are bound by reading K and
+// V: the rows are the columns of a wave's matrix tiles (tree_wave.h), K and V go from memory into
+// registers once for all of them, and the keys of all sequences are shared out as those of cross attention
+// are (rows_kernel.h). Any other batch runs on the row tiles of the prefill kernel (attn.hip) with bits
+// for the causal bound.
 #include <algorithm>
-#include <type_traits>
 
 #include "pcr_internal.h"
-#include "tree_wave.h"
 
 namespace pcr {
 namespace {
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short u16;
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kStepKeys = tree_wave::kStepKeys;
-
-struct TreeArgs {
-    int32_t num_blocks, Hkv, Hq, max_blocks, B, T, words;
-    float scale_log2;
-};
-
-// Grid (row groups, kv heads, sequences).
-template <int D, int NC, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1))) void tree_rows_kernel(
-    const TreeArgs a, const u16 *__restrict__ q, const u16 *__restrict__ pool_k, const u16 *__restrict__ pool_v,
-    const int32_t *__restrict__ block_tables, const int32_t *__restrict__ prefix_lens,
-    const int32_t *__restrict__ cu_nodes, const uint64_t *__restrict__ visible, u16 *__restrict__ out)
-{
-    constexpr int MT = D / 16;
-    __shared__ f32x4 part_o[WAVES - 1][NC][MT][64];
-    __shared__ f32x2 part_ml[WAVES - 1][NC][64];
-    const int lane = threadIdx.x & 63, c = lane & 15, q4 = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int g = blockIdx.y, b = blockIdx.z, G = a.Hq / a.Hkv;
-    const int t0 = cu_nodes[b], nodes = min(cu_nodes[b + 1], a.T) - t0, prefix = prefix_lens[b];
-    if (t0 < 0 || nodes <= 0 || prefix < 0) return;
-    tree_wave::Rows rw{visible + (int64_t)t0 * a.words, a.words, prefix, nodes, (int)blockIdx.x * 16 * NC, 0, G};
-    rw.rows = nodes * G - rw.row0;
-    if (rw.rows <= 0) return;
-    const int n_keys = (int)min((int64_t)prefix + nodes, (int64_t)a.max_blocks * kBlockSize);
-    const int steps = (n_keys + kStepKeys - 1) / kStepKeys, per = (steps + WAVES - 1) / WAVES;
-    const int kbeg = wave * per * kStepKeys, kend = min(n_keys, kbeg + per * kStepKeys);
-    f32x4 o[NC][MT];
-    float m[NC], l[NC];
-    if (kbeg < kend) {
-        tree_wave::chunk<D, NC, 2, true>(q + ((int64_t)t0 * a.Hq + g * G) * D, (int64_t)a.Hq * D, rw, pool_k, pool_v,
-                                         a.num_blocks, a.Hkv, g, block_tables + (int64_t)b * a.max_blocks,
-                                         (n_keys - 1) >> 4, kbeg, kend, a.scale_log2, o, m, l);
-    } else {
-#pragma unroll
-        for (int t = 0; t < NC; ++t) {
-            m[t] = tree_wave::kNoMax;
-            l[t] = 0.f;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) o[t][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < NC; ++t) {
-        l[t] += __shfl_xor(l[t], 16);
-        l[t] += __shfl_xor(l[t], 32);
-    }
-    // Waves 1.. leave O (lane layout), max and sum in LDS; wave 0 merges.
-    if (wave > 0) {
-#pragma unroll
-        for (int t = 0; t < NC; ++t) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) part_o[wave - 1][t][mt][lane] = o[t][mt];
-            part_ml[wave - 1][t][lane] = f32x2{m[t], l[t]};
-        }
-    }
-    __syncthreads();
-    if (wave > 0) return;
-#pragma unroll
-    for (int t = 0; t < NC; ++t) {
-        float M = m[t];
-        for (int w = 0; w < WAVES - 1; ++w) M = fmaxf(M, part_ml[w][t][lane][0]);
-        const float a0 = __builtin_amdgcn_exp2f(m[t] - M);
-        float L = l[t] * a0;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) o[t][mt] *= a0;
-        for (int w = 0; w < WAVES - 1; ++w) {
-            const f32x2 ml = part_ml[w][t][lane];
-            const float aw = __builtin_amdgcn_exp2f(ml[0] - M);
-            L += aw * ml[1];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) o[t][mt] += aw * part_o[w][t][mt][lane];
-        }
-        const int r = 16 * t + c;
-        if (r >= rw.rows) continue;
-        const int pr = rw.row0 + r, node = pr / G, h = pr - node * G;
-        const float inv = L == 0.f ? 0.f : 1.f / L;     // a row that sees nothing is zeros
-        u16 *orow = out + ((int64_t)(t0 + node) * a.Hq + g * G + h) * D + 4 * q4;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const bf16x4 v = __builtin_convertvector(o[t][mt] * inv, bf16x4);
-            *reinterpret_cast<u32x2 *>(orow + 16 * mt) = __builtin_bit_cast(u32x2, v);
-        }
-    }
-}
-
 constexpr int32_t kMaxKeys = 1 << 30;       // positions past a sequence's end still fit int32
+constexpr int kMaxRows = kTreeMaxCols;      // packed rows of a sequence up to which waves hold them as columns
+
+// 32-key steps of n keys (tree_wave.h).
+int64_t key_steps(int64_t n) { return (n + 31) / 32; }
+
+pcr_status check_workspace(int64_t need, const void *workspace, int64_t bytes, const char *who)
+{
+    if (need == 0) return PCR_OK;
+    if (!workspace || bytes < need)
+        return fail(PCR_ERR_INVALID_ARG, "%s: this batch needs a workspace of %lld bytes (%lld given)", who,
+                    (long long)need, (long long)(workspace ? bytes : 0));
+    if ((uintptr_t)workspace & 15) return fail(PCR_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+    return PCR_OK;
+}
 
 pcr_status check_heads(int32_t num_q_heads, int32_t num_kv_heads, const char *who)
 {
@@ -138,6 +58,16 @@ pcr_status pcr_tree_attn_workspace_size(int32_t B, int32_t total_nodes, int32_t 
     if (st) return st;
     if (B < 0 || total_nodes < 0 || max_keys < 0)
         return fail(PCR_ERR_INVALID_ARG, "%s: negative B, total_nodes or max_keys", who);
+    if (B == 0 || total_nodes == 0 || max_keys == 0) return PCR_OK;
+    int32_t n_cu = 0;
+    st = device_cu_count(&n_cu, who);
+    if (st) return st;
+    const int64_t rows = (int64_t)total_nodes * (num_q_heads / num_kv_heads);
+    const int32_t cols = (int32_t)std::min<int64_t>(rows, kMaxRows);
+    // (sequences without nodes count: a plan of parts has slots for them too)
+    const int64_t steps = (int64_t)B * num_kv_heads * key_steps(max_keys);
+    *bytes = cross_rows_workspace_bytes(std::min(steps, cross_rows_max_slots(head_dim, n_cu)), cols, head_dim);
+    if (rows > kMaxRows) *bytes = std::max(*bytes, cross_tiles_workspace_bytes());
     return PCR_OK;
 }
 
@@ -161,8 +91,12 @@ pcr_status pcr_tree_attn(const void *q, const pcr_kv_pool *pool, const int32_t *
         return fail(PCR_ERR_UNSUPPORTED, "%s: mask_words %d is not in 1 .. %d", who, mask_words, kMaxMaskWords);
     if (host_cu_nodes[0] != 0) return fail(PCR_ERR_INVALID_ARG, "%s: cu_nodes[0] must be 0", who);
     const int D = pool->head_dim, G = num_q_heads / pool->num_kv_heads;
-    if (B > 65535 || pool->num_kv_heads > 65535) return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
+    if ((int64_t)B * pool->num_kv_heads > (int64_t)1 << 22)
+        return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
     int64_t most = 0;                       // packed rows of a sequence, at most
+    int64_t steps = 0;                      // 32-key steps of all (sequence, kv head) pairs with rows
+    int64_t longest = 0;                    // of one of them, at most
+    int64_t tiles = 0;                      // row tiles of one kv head
     for (int32_t b = 0; b < B; ++b) {
         const int64_t n = (int64_t)host_cu_nodes[b + 1] - host_cu_nodes[b];
         if (n < 0 || host_prefix_lens[b] < 0)
@@ -176,6 +110,12 @@ pcr_status pcr_tree_attn(const void *q, const pcr_kv_pool *pool, const int32_t *
             return fail(PCR_ERR_INVALID_ARG, "%s: sequence %d needs more blocks than max_blocks %d", who, b,
                         max_blocks);
         most = std::max(most, n * G);
+        if (n > 0) {
+            const int64_t st_b = key_steps(host_prefix_lens[b] + n);
+            steps += st_b * pool->num_kv_heads;
+            longest = std::max(longest, st_b);
+        }
+        tiles += (n * G + attn_rows_per_workgroup(D) - 1) / attn_rows_per_workgroup(D);
     }
     const int64_t T = host_cu_nodes[B];
     if (T == 0) return PCR_OK;
@@ -187,22 +127,41 @@ pcr_status pcr_tree_attn(const void *q, const pcr_kv_pool *pool, const int32_t *
     if ((uintptr_t)visible & 7) return fail(PCR_ERR_INVALID_ARG, "%s: visible must be 8-byte aligned", who);
     const uintptr_t qa = (uintptr_t)q, oa = (uintptr_t)out, bytes = (uintptr_t)T * num_q_heads * D * 2;
     if (qa < oa + bytes && oa < qa + bytes) return fail(PCR_ERR_INVALID_ARG, "%s: q and out overlap", who);
-    TreeArgs a{pool->num_blocks, pool->num_kv_heads, num_q_heads, max_blocks, B, (int32_t)T, mask_words,
-               sm_scale * kLog2e};
-    auto go = [&](auto dim, auto tiles) {
-        constexpr int DD = decltype(dim)::value, NC = decltype(tiles)::value;
-        const dim3 grid((unsigned)((most + 16 * NC - 1) / (16 * NC)), pool->num_kv_heads, B);
-        hipLaunchKernelGGL((tree_rows_kernel<DD, NC, 4>), grid, dim3(256), 0, static_cast<hipStream_t>(stream), a,
-                           static_cast<const u16 *>(q), static_cast<const u16 *>(pool->k),
-                           static_cast<const u16 *>(pool->v), block_tables, prefix_lens, cu_nodes, visible,
-                           static_cast<u16 *>(out));
-        return hipGetLastError();
-    };
-    auto go_d = [&](auto dim) {
-        if (most <= 16) return go(dim, std::integral_constant<int, 1>{});
-        return go(dim, std::integral_constant<int, 2>{});
-    };
-    const hipError_t e = D == 128 ? go_d(std::integral_constant<int, 128>{}) : go_d(std::integral_constant<int, 64>{});
+    int32_t n_cu = 0;
+    st = device_cu_count(&n_cu, who);
+    if (st) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    if (most <= kMaxRows) {
+        if (steps > INT32_MAX) return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
+        // Constants for two sets of registers where cross attention has three (one sequence, four nodes of 32 / 8
+        // heads of 128 over 500 and 2000 keys: whole pairs 13.5 and 26.9 us, eight parts 13.8 and 15.2; 8 / 8 heads of
+        // 64 over 1000 and 4000: 11.5 and 24.1, 14.3 and 13.9). Two tiles of columns leave twice the partial
+        // results (64 ragged sequences of up to 4096 keys, eight nodes of 32 / 8 heads: even runs 142 us, whole pairs 133).
+        const CrossRowsPlan plan = rows_plan(steps, (int64_t)B * pool->num_kv_heads, longest, D, n_cu,
+                                             {D == 128 ? 0.29f : 0.15f, 11.f, most > 16 ? 1.25f : 1.f});
+        bool cut = plan.parts > 1;          // some (sequence, kv head) lies in two runs
+        int64_t x = 0;
+        for (int32_t b = 0; b < B && !cut && !plan.parts; ++b) {
+            const int64_t n = host_cu_nodes[b + 1] - host_cu_nodes[b];
+            const int64_t st_b = n > 0 ? key_steps(host_prefix_lens[b] + n) : 0;
+            for (int32_t g = 0; st_b > 0 && g < pool->num_kv_heads && !cut; ++g, x += st_b)
+                cut = cross_rows_run(plan, steps, x) != cross_rows_run(plan, steps, x + st_b - 1);
+        }
+        st = check_workspace(cut ? cross_rows_workspace_bytes(plan.slots, (int32_t)most, D) : 0, workspace,
+                             workspace_bytes, who);
+        if (st) return st;
+        e = launch_tree_rows(q, *pool, block_tables, max_blocks, prefix_lens, cu_nodes, B, visible, mask_words,
+                             num_q_heads, (int32_t)T, (int32_t)most, steps, plan, cut, sm_scale, out, workspace, s);
+    } else {
+        if (tiles * pool->num_kv_heads > (int64_t)1 << 22) return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
+        // The partial results of a key split, asked for whether or not this batch takes one, as the size
+        // query, which does not know the lengths, does.
+        st = check_workspace(cross_tiles_workspace_bytes(), workspace, workspace_bytes, who);
+        if (st) return st;
+        e = launch_tree_tiles(q, *pool, block_tables, max_blocks, host_prefix_lens, host_cu_nodes, B, visible,
+                              mask_words, num_q_heads, (int32_t)T, sm_scale, out, workspace, s, n_cu);
+    }
     if (e != hipSuccess) return hip_fail(e, "pcr_tree_attn: launch");
     return PCR_OK;
 }

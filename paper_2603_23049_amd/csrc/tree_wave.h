@@ -50,13 +50,13 @@ struct Rows {
     const uint64_t *visible;      // words of the sequence's first node
     int32_t n_words;
     int32_t prefix, nodes;
-    int32_t row0, rows;           // first packed row, and how many from it on (may be more than 16 NC)
+    int32_t rows;                 // packed rows, up to 16 NC
     int32_t G;
 };
 
 // q: the sequence's first node's first head of this kv head; q_stride: elements from node to node.
 // bt_row: the sequence's block-table row; last_blk: its last block with a key.
-template <int D, int NC, int NSETS, bool K_CACHED>
+template <int D, int NC, bool K_CACHED>
 __device__ __forceinline__ void chunk(const u16 *__restrict__ q, int64_t q_stride, const Rows &rw,
                                       const u16 *__restrict__ pool_k, const u16 *__restrict__ pool_v,
                                       int32_t num_blocks, int32_t Hkv, int g, const int32_t *__restrict__ bt_row,
@@ -73,7 +73,7 @@ __device__ __forceinline__ void chunk(const u16 *__restrict__ q, int64_t q_strid
     for (int t = 0; t < NC; ++t) {
         const int r = 16 * t + c;
         const bool col = r < rw.rows;
-        const int pr = rw.row0 + (col ? r : 0), node = pr / rw.G, h = pr - node * rw.G;
+        const int pr = col ? r : 0, node = pr / rw.G, h = pr - node * rw.G;
         const u16 *qrow = q + (int64_t)node * q_stride + h * D + 8 * q4;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
@@ -93,13 +93,8 @@ __device__ __forceinline__ void chunk(const u16 *__restrict__ q, int64_t q_strid
         const int32_t vb = (q4 >> 1) ? b1 : b0;
         const u16 *vp = pool_v + ((int64_t)vb * Hkv + g) * (kBlockSize * D) + c * kBlockSize + 8 * (q4 & 1);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const u32x4 *vq = reinterpret_cast<const u32x4 *>(vp + 16 * mt * kBlockSize);
-            if constexpr (K_CACHED)
-                R.v[mt] = *vq;
-            else
-                R.v[mt] = __builtin_nontemporal_load(vq);
-        }
+        for (int mt = 0; mt < MT; ++mt)
+            R.v[mt] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + 16 * mt * kBlockSize));
     };
     auto load_step = [&](int step, StepRegs<D> &R) __attribute__((always_inline)) {
         const int li = (kbeg + step * kStepKeys) >> 4;
@@ -202,7 +197,7 @@ __device__ __forceinline__ void chunk(const u16 *__restrict__ q, int64_t q_strid
 #pragma unroll
         for (int t = 0; t < NC; ++t) {
             const int r = 16 * t + c;
-            const int node = (rw.row0 + (r < rw.rows ? r : 0)) / rw.G;
+            const int node = (r < rw.rows ? r : 0) / rw.G;
             unsigned seen = seen8(rw.visible + (int64_t)node * rw.n_words, rw.n_words, k0 - rw.prefix, rw.nodes);
             if (kend - k0 < 8) seen &= kend > k0 ? (1u << (kend - k0)) - 1 : 0u;
             __builtin_amdgcn_sched_barrier(0);
@@ -247,28 +242,30 @@ __device__ __forceinline__ void chunk(const u16 *__restrict__ q, int64_t q_strid
         }
     };
 
-    // Steps of cached keys only, with the next step's loads in flight; then the others.
+    // Every load is unconditional (a step index past the end rereads the last step). Full steps of cached
+    // keys first, the two sets of registers taking turns; then the others, one at a time. (A third set, as in
+    // decode_wave.h, took more: one node's four heads of 64 sequences of 500-4096 keys 123 us with two sets and 127
+    // with three, two tiles of columns 141 and 172.)
     const int n_steps = (kend - kbeg + kStepKeys - 1) / kStepKeys;
     const int n_plain = max(0, min(kend, rw.prefix) - kbeg) / kStepKeys;
-    static_assert(NSETS == 2, "two register sets");
+    auto load = [&](int j, StepRegs<D> &R) __attribute__((always_inline)) { load_step(min(j, n_steps - 1), R); };
     StepRegs<D> ra, rb;
-    load_step(0, ra);
+    load(0, ra);
     int j = 0;
     for (; j + 2 <= n_plain; j += 2) {
-        load_step(min(j + 1, n_steps - 1), rb);
+        load(j + 1, rb);
         process(ra);
-        load_step(min(j + 2, n_steps - 1), ra);
+        load(j + 2, ra);
         process(rb);
     }
     if (j < n_plain) {
-        load_step(min(j + 1, n_steps - 1), rb);
+        load(++j, rb);
         process(ra);
-        ++j;
         ra = rb;
     }
 #pragma unroll 1
     for (; j < n_steps; ++j) {
-        load_step(min(j + 1, n_steps - 1), rb);
+        load(j + 1, rb);
         process_masked(j, ra);
         ra = rb;
     }
