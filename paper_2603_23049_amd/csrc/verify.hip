@@ -213,47 +213,70 @@ __device__ __forceinline__ void values(const Row &r, const Four &x, int32_t base
     }
 }
 
-// A wave's share of a pass: the tiles first, first + step, .. in pieces; AHEAD: the next one's loads in flight
-// while one is added.
+// Sum of what is left of the vectors v .. of a piece (all lanes of a wave).
+template <int N>
+__device__ __forceinline__ double piece_sum(const VerifyArgs &a, const Row &r, int32_t base, const Four (&x)[N])
+{
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        double e[4];
+        const int32_t at = base + k * 256;
+        values(r, x[k], at, at + 4 * (int32_t)(threadIdx.x & 63), a.V, e);
+        s += (e[0] + e[1]) + (e[2] + e[3]);
+    }
+    return s;
+}
+template <int N>
+__device__ __forceinline__ void load_piece(const VerifyArgs &a, const Row &r, int32_t base, Four (&x)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = load(r, a.V, base + k * 256 + 4 * (int32_t)(threadIdx.x & 63));
+}
+// First element of a tile's piece (the row's end where it lies past it: no element of it).
+__device__ __forceinline__ int32_t piece_begin(const VerifyArgs &a, int32_t t, int32_t piece)
+{
+    return (int32_t)min(((int64_t)t * a.pieces + piece) * kPiece, (int64_t)a.V);
+}
+
+// A wave's share of a pass: the tiles first, first + step, .. in pieces. AHEAD: the next piece's loads are in flight
+// while one is added (a workgroup alone on its compute unit); else many waves hide them.
 template <bool AHEAD>
 __device__ __forceinline__ void tile_sums(const VerifyArgs &a, const Row &r, int32_t first, int32_t step, double *sums)
 {
-    if (first >= a.tiles) return;
     const int lane = threadIdx.x & 63;
-    auto begin = [&](int32_t t, int32_t piece) {            // (past the row's end: no element of it)
-        return (int32_t)min(((int64_t)t * a.pieces + piece) * kPiece, (int64_t)a.V);
-    };
-    Four x[kVecs], y[kVecs];
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) x[k] = load(r, a.V, begin(first, 0) + k * 256 + 4 * lane);
-    double s = 0.0;
-    for (int32_t t = first, piece = 0; t < a.tiles;) {
-        const int32_t base = begin(t, piece);
-        const bool ends = piece + 1 == a.pieces;
-        const int32_t t2 = ends ? t + step : t, piece2 = ends ? 0 : piece + 1;
-        if (AHEAD && t2 < a.tiles) {
-#pragma unroll
-            for (int k = 0; k < kVecs; ++k) y[k] = load(r, a.V, begin(t2, piece2) + k * 256 + 4 * lane);
-        }
-#pragma unroll
-        for (int k = 0; k < kVecs; ++k) {
-            double e[4];
-            values(r, x[k], base + k * 256, base + k * 256 + 4 * lane, a.V, e);
-            s += (e[0] + e[1]) + (e[2] + e[3]);
-        }
-        if (ends) {
+    if constexpr (!AHEAD) {
+        for (int32_t t = first; t < a.tiles; t += step) {
+            double s = 0.0;
+            for (int32_t piece = 0; piece < a.pieces; ++piece) {
+                Four x[kVecs];
+                const int32_t base = piece_begin(a, t, piece);
+                load_piece(a, r, base, x);
+                s += piece_sum(a, r, base, x);
+            }
             s = wave_sum(s);
             if (lane == 0) sums[t] = s;
-            s = 0.0;
         }
-        if (!AHEAD && t2 < a.tiles) {
+    } else {
+        if (first >= a.tiles) return;
+        Four x[kVecs], y[kVecs];
+        load_piece(a, r, piece_begin(a, first, 0), x);
+        double s = 0.0;
+        for (int32_t t = first, piece = 0; t < a.tiles;) {
+            const bool ends = piece + 1 == a.pieces;
+            const int32_t t2 = ends ? t + step : t, piece2 = ends ? 0 : piece + 1;
+            if (t2 < a.tiles) load_piece(a, r, piece_begin(a, t2, piece2), y);
+            s += piece_sum(a, r, piece_begin(a, t, piece), x);
+            if (ends) {
+                s = wave_sum(s);
+                if (lane == 0) sums[t] = s;
+                s = 0.0;
+            }
 #pragma unroll
-            for (int k = 0; k < kVecs; ++k) y[k] = load(r, a.V, begin(t2, piece2) + k * 256 + 4 * lane);
+            for (int k = 0; k < kVecs; ++k) x[k] = y[k];
+            t = t2;
+            piece = piece2;
         }
-#pragma unroll
-        for (int k = 0; k < kVecs; ++k) x[k] = y[k];
-        t = t2;
-        piece = piece2;
     }
 }
 
