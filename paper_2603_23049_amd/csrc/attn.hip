@@ -1334,7 +1334,8 @@ __global__ __launch_bounds__(kCombineThreads) void split_combine_kernel(int32_t 
                         const float w = k0 + i < ns && ml[i][0] != -INFINITY
                                             ? __builtin_amdgcn_exp2f((ml[i][0] - M) * c) : 0.f;
                         L += w * ml[i][1];
-                        acc += w * o[i];
+                        // (a tree's chunk may hold infinities: its reread copy, of weight 0, adds nothing)
+                        if (!TREE || w > 0.f) acc += w * o[i];
                     }
                 }
             };

@@ -330,7 +330,8 @@ __global__ __launch_bounds__(64 * kCombineWaves) void cross_rows_combine_kernel(
                     float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(j0 + i, 63)));
                 const float wv = j0 + i < np ? wi : 0.f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] += wv * po[i][e];
+                for (int e = 0; e < E; ++e)              // (a tree's part may hold infinities: reread, it adds nothing)
+                    if (!TREE || wv > 0.f) acc[e] += wv * po[i][e];
             }
         }
     }

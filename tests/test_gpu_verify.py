@@ -152,6 +152,25 @@ def test_same_token_twice():
 
 
 @pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("V", [300, 20011])
+def test_many_children(V, drawn):
+    """Hundreds of children of one node, nearly all refused (they lie in several 64s of nodes), and a
+    chain behind the last one."""
+    c = Case([330, 200], V, drawn, 17, back=1)
+    for b, n in enumerate(c.n):
+        t0 = c.cu[b]
+        c.parents[t0 + 1:t0 + n] = 0
+        c.parents[t0 + n - 2], c.parents[t0 + n - 1] = n - 3, n - 2
+        if not drawn:
+            order = np.argsort(c.target[t0])                 # the least likely tokens, each once
+            c.tokens[t0 + 1:t0 + n] = np.resize(order[:max(64, V // 2)], n - 1)
+    c.uniforms[:] = np.maximum(c.uniforms, 0.3)
+    got = c.check()
+    c.uniforms[[0, 330]] = [0.0, 1 - 2.0 ** -24]
+    c.check()
+
+
+@pytest.mark.parametrize("drawn", [True, False])
 def test_distribution(drawn):
     """The first new token is distributed as the target's first row, whatever the draft: over N draws a
     token's count is within 5 sqrt(N p (1 - p)) + 1 of N p (a deviation of 5 sigma: below 1e-6 each)."""
