@@ -17,7 +17,7 @@ namespace pcr {
 // plan, 37% at best; the worst, a call of 14 us, 14% more.)
 CrossRowsPlan cross_rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu)
 {
-    return rows_plan(steps, pairs, longest, head_dim, n_cu, {head_dim == 128 ? 0.41f : 0.22f, 9.5f, 1.f});
+    return rows_plan(steps, pairs, longest, head_dim, n_cu, {head_dim == 128 ? 0.41f : 0.22f, 9.5f, 1.f, 8});
 }
 
 CrossRowsPlan rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu,
@@ -43,7 +43,7 @@ CrossRowsPlan rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t h
     const float even = (four ? 13.5f : 11.f + 3.f * std::min(1.f, single / 600.f)) + bw * cost.even;
     if (whole <= even && (k == 1 || whole <= parts)) {
         p.parts = 1;
-        p.waves = !wide && pairs * 8 <= waves ? 8 : pairs * 4 <= waves ? 4 : pairs * 2 <= waves ? 2 : 1;
+        p.waves = !wide && cost.waves == 8 && pairs * 8 <= waves ? 8 : pairs * 4 <= waves ? 4 : pairs * 2 <= waves ? 2 : 1;
         // more pairs than waves: long ones are shared all the same, so that the last ends earlier
         if (p.waves == 1 && longest >= (wide ? 64 : 20)) p.waves = 4;
         p.runs = (int32_t)pairs;

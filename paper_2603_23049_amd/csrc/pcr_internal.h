@@ -103,9 +103,10 @@ struct CrossRowsPlan {
 // pairs: of all sequences (those without steps too); longest: steps of one pair, at most.
 CrossRowsPlan cross_rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu);
 // The same with the estimate's constants: us of a compute unit for a step, what parts take with nothing to
-// read, and how much longer than other cuts even runs take to read.
+// read, how much longer than other cuts even runs take to read, and the most waves of a whole pair.
 struct RowsCost {
     float cu, parts, even;
+    int32_t waves;
 };
 CrossRowsPlan rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu,
                         const RowsCost &cost);

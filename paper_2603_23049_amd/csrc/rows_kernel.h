@@ -386,7 +386,7 @@ hipError_t launch_rows(const void *q, const pcr_kv_pool &pool, const int32_t *bl
             rows(cross_rows_kernel<D, 2, kWhole, NC>);
         } else if (plan.waves == 1) {
             rows(cross_rows_kernel<D, 1, kWhole, NC>);
-        } else if constexpr (D == 64) {
+        } else if constexpr (D == 64 && NC == 0) {
             rows(cross_rows_kernel<D, 8, kWhole, NC>);
         }
         const hipError_t e = hipGetLastError();

@@ -33,12 +33,16 @@ struct StepRegs {
     u32x4 v[D / 16];      // V^T operands (dims 16*mt ..)
 };
 
-// Bits [d, d + 8) of a row's words, where bits below 0 are set and those from n on are not.
-__device__ __forceinline__ unsigned seen8(const uint64_t *__restrict__ words, int32_t n_words, int d, int n)
+// Bits [d, d + 8) of a row's words (the first of them in a register), where bits below 0 are set and those
+// from n on are not.
+__device__ __forceinline__ unsigned seen8(const uint64_t *__restrict__ words, uint64_t first, int32_t n_words, int d, int n)
 {
     const int lo = max(d, 0), w = lo >> 6, sh = lo & 63;
-    uint64_t x = w < n_words ? words[w] >> sh : 0ull;
-    if (sh > 56 && w + 1 < n_words) x |= words[w + 1] << (64 - sh);
+    uint64_t x = w == 0 ? first >> sh : 0ull;
+    if (n_words > 1) {                                  // wave-uniform
+        if (w > 0 && w < n_words) x = words[w] >> sh;
+        if (sh > 56 && w + 1 < n_words) x |= words[w + 1] << (64 - sh);
+    }
     const int cached = min(lo - d, 8);                  // bits below 0
     unsigned bits = cached == 8 ? 0xFFu : (((unsigned)x << cached) | ((1u << cached) - 1)) & 0xFFu;
     if (d + 8 > n) bits &= n > d ? (1u << (n - d)) - 1 : 0u;
@@ -69,11 +73,13 @@ __device__ __forceinline__ void chunk(const u16 *__restrict__ q, int64_t q_strid
 
     // Q^T operands: lane (c, q4) holds dims 32*kk + 8*q4 .. +7 of its row (zero past the last).
     u32x4 qf[NC][KK];
+    uint64_t first[NC];           // the rows' first words, asked for here: a load in the step waits a microsecond
 #pragma unroll
     for (int t = 0; t < NC; ++t) {
         const int r = 16 * t + c;
         const bool col = r < rw.rows;
         const int pr = col ? r : 0, node = pr / rw.G, h = pr - node * rw.G;
+        first[t] = rw.visible[(int64_t)node * rw.n_words];
         const u16 *qrow = q + (int64_t)node * q_stride + h * D + 8 * q4;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
@@ -198,7 +204,7 @@ __device__ __forceinline__ void chunk(const u16 *__restrict__ q, int64_t q_strid
         for (int t = 0; t < NC; ++t) {
             const int r = 16 * t + c;
             const int node = (r < rw.rows ? r : 0) / rw.G;
-            unsigned seen = seen8(rw.visible + (int64_t)node * rw.n_words, rw.n_words, k0 - rw.prefix, rw.nodes);
+            unsigned seen = seen8(rw.visible + (int64_t)node * rw.n_words, first[t], rw.n_words, k0 - rw.prefix, rw.nodes);
             if (kend - k0 < 8) seen &= kend > k0 ? (1u << (kend - k0)) - 1 : 0u;
             __builtin_amdgcn_sched_barrier(0);
             pb[t] = probabilities(t, R, seen, true);
