@@ -25,7 +25,7 @@ FORMS = [
     ([12000] + [900] * 6, 2, 2, 1, 64), (_spread(5, 100, 998, 2, 13410), 5, 4, 1, 64),   # of four
     ([3840], 4, 1, 1, 128), ([6675], 9, 2, 1, 128),
     ([2080], 16, 1, 1, 64), ([2080], 8, 4, 1, 64), ([2080], 2, 8, 1, 128), ([2080], 4, 8, 1, 128),   # parts of a pair
-    ([20], 5, 8, 8, 64), ([3], 17, 8, 8, 64), ([0], 5, 4, 2, 128), ([30], 9, 4, 2, 128),        # whole pairs, eight and four waves
+    ([20], 5, 8, 8, 64), ([3], 17, 8, 8, 64), ([0], 5, 4, 2, 128), ([30], 9, 4, 2, 128),        # whole pairs, four waves
     (_spread(260, 1, 12, 3), 2, 4, 1, 64), (_spread(257, 0, 12, 4), 3, 8, 1, 64),
     (_spread(69, 0, 14, 5), 1, 16, 8, 64), (_spread(66, 0, 14, 6), 3, 64, 8, 64),             # two waves
     (_spread(34, 0, 14, 7), 2, 16, 8, 128), (_spread(33, 0, 14, 8), 3, 64, 8, 128),
