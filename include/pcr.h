@@ -262,7 +262,7 @@ pcr_status pcr_prefix_prefill_attn(const void *q, const pcr_kv_pool *pool,
 
 /*
  * pcr_prefill_attn_set_schedule -- how pcr_prefix_prefill_attn (and the pipelines'
- * attention, and pcr_cross_attn with more than 16 packed rows in a sequence) divides a launch
+ * attention, pcr_cross_attn with more than 16 packed rows in a sequence and pcr_tree_attn with more than 32) divides a launch
  * among workgroups; a tuning and testing control, not part of the method. Every schedule
  * computes the same result (Sec. 2.2).
  *   PCR_ATTN_SCHEDULE_AUTO (the default): row halves from two of their workgroups per
@@ -652,9 +652,9 @@ pcr_status pcr_tree_attn_workspace_size(int32_t B, int32_t total_nodes, int32_t 
  *                  pcr_verify_drafts_workspace_size bytes (NULL when that is 0); scratch. One
  *                  workspace serves every call ordered on one stream; calls that may overlap
  *                  (captured graphs that may run together among them) need their own.
- * Probabilities that are negative or NaN count as 0; rows need not sum to one exactly. Sums are
- * fp64, products and differences rounded one by one, in an order that is fixed for a given B and vocab:
- * repeated calls give the same tokens. No other overlap of outputs. Errors: PCR_ERR_INVALID_ARG for
+ * A remainder r(v) that is negative or NaN counts as 0; rows need not sum to one exactly. Sums are
+ * fp64, products and differences rounded one by one, in an order that the vocabulary alone fixes:
+ * repeated calls, and a sequence alone or among others, give the same tokens. No other overlap of outputs. Errors: PCR_ERR_INVALID_ARG for
  * negative counts, vocab or path_cap < 1, strides below vocab, NULL arrays, a workspace that is
  * missing, misaligned or too small; PCR_ERR_UNSUPPORTED beyond 2^21 sequences, 2^27 nodes, a
  * vocabulary of 2^30 or strides of 2^32.

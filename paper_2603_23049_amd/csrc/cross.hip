@@ -45,24 +45,6 @@ constexpr int32_t kMaxKeys = 1 << 30;       // positions past a sequence's end s
 // 32-key steps of n keys (decode_wave.h).
 int64_t key_steps(int32_t n) { return ((int64_t)n + 31) / 32; }
 
-pcr_status check_workspace(int64_t need, const void *workspace, int64_t bytes, const char *who)
-{
-    if (need == 0) return PCR_OK;
-    if (!workspace || bytes < need)
-        return fail(PCR_ERR_INVALID_ARG, "%s: this batch needs a workspace of %lld bytes (%lld given)", who,
-                    (long long)need, (long long)(workspace ? bytes : 0));
-    if ((uintptr_t)workspace & 15) return fail(PCR_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
-    return PCR_OK;
-}
-
-pcr_status check_heads(int32_t num_q_heads, int32_t num_kv_heads, const char *who)
-{
-    if (num_q_heads <= 0 || num_q_heads % num_kv_heads != 0)
-        return fail(PCR_ERR_UNSUPPORTED, "%s: num_q_heads %d is not a positive multiple of num_kv_heads %d", who,
-                    num_q_heads, num_kv_heads);
-    return PCR_OK;
-}
-
 }  // namespace
 }  // namespace pcr
 

@@ -18,6 +18,9 @@ void clear_error();
 // The checks every entry point makes of a block layout and of a pool (errors name `who`).
 pcr_status check_layout(int32_t block_size, int32_t num_kv_heads, int32_t head_dim, const char *who);
 pcr_status check_pool(const pcr_kv_pool *pool, const char *who);
+// Query heads of a pool with num_kv_heads, and a caller's workspace of which `need` bytes are needed.
+pcr_status check_heads(int32_t num_q_heads, int32_t num_kv_heads, const char *who);
+pcr_status check_workspace(int64_t need, const void *workspace, int64_t bytes, const char *who);
 
 // Up to this many (src, dst) block pairs travel in one pull-kernel launch as
 // kernel arguments (so no device copy of the host lists is needed).

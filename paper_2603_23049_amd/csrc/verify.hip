@@ -14,7 +14,9 @@
 // which several workgroups per sequence each walk as far as the walk goes without a new sum (the
 // walk itself is a few dependent loads) and then sum their tiles of the row it needs. The last
 // launch, one workgroup per sequence, ends the walk (with passes of its own where a walk needs more
-// rounds than were launched) and draws: the tile sums lead to the tile, which is read once more.
+// rounds than were launched) and draws: the tile sums lead to the tile, which is read once more. (64 chains of
+// 4 over 128000 tokens: a round 13.5 us, of which the rows' 57 MB take 9 and the walk before them four
+// dependent loads; the draw 8.3, dependent loads too.)
 #include <algorithm>
 
 #include "pcr_internal.h"
@@ -533,13 +535,8 @@ pcr_status pcr_verify_drafts(int32_t B, const int32_t *cu_nodes, const int32_t *
         (T > 0 && (!parents || !tokens || !target_probs || !uniforms)))
         return fail(PCR_ERR_INVALID_ARG, "%s: NULL argument", who);
     const Plan plan = make_plan(B, T, vocab, draft_probs != nullptr);
-    if (plan.bytes > 0) {
-        if (!workspace || workspace_bytes < plan.bytes)
-            return fail(PCR_ERR_INVALID_ARG, "%s: this batch needs a workspace of %lld bytes (%lld given)", who,
-                        (long long)plan.bytes, (long long)(workspace ? workspace_bytes : 0));
-        if ((uintptr_t)workspace & 15)
-            return fail(PCR_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
-    }
+    const pcr_status st = check_workspace(plan.bytes, workspace, workspace_bytes, who);
+    if (st) return st;
     State *states = static_cast<State *>(workspace);
     const VerifyArgs a{cu_nodes, parents, tokens, prefix_lens, target_probs, draft_probs, uniforms, target_stride,
                        draft_stride, path, accepted_lens, next_tokens, context_lens, B, T, vocab, path_cap, plan.tiles,

@@ -50,7 +50,7 @@ def test_every_form_is_tested_and_resident():
     assert len(built) == 24
     assert {_form(*f) for f in forms.FORMS} == set(built)
     for (d, waves, cut, tiles), r in built.items():
-        assert r["Occupancy"] >= (1 if d == 128 or tiles > 1 else 2), (d, waves, cut, tiles, r)
+        assert r["Occupancy"] >= (1 if d == 128 else 2), (d, waves, cut, tiles, r)   # as the plan counts them
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not installed")
