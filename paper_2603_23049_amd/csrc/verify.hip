@@ -490,7 +490,11 @@ Plan make_plan(int32_t B, int32_t T, int32_t V, bool drawn)
     p.tiles = (int32_t)((V + size - 1) / size);
     const int64_t nodes = ((int64_t)T + std::max(B, 1) - 1) / std::max(B, 1);
     p.rounds = p.tiles <= 8 || B > kRoundSeqs ? 0 : !drawn || nodes <= 5 || p.tiles < 48 ? 1 : nodes <= 9 ? 2 : 4;
-    p.wgs = (int32_t)std::min<int64_t>((p.tiles + kRoundWaves - 1) / kRoundWaves, std::max<int64_t>(1, 4096 / std::max(B, 1)));
+    // Two tiles a wave where the sequences fill the device that way, one where they are fewer, more where they
+    // are many (64 chains of 4, 128000 tokens: one tile a wave 24.7 us, two 22.7; 128 trees of 12: 67.6 and 68.1,
+    // four 74.8).
+    const int64_t seqs = std::max(B, 1), one = (p.tiles + kRoundWaves - 1) / kRoundWaves, two = (one + 1) / 2;
+    p.wgs = (int32_t)std::max<int64_t>(1, std::min(one, std::max(1024 / seqs, std::min(two, 4096 / seqs))));
     p.bytes = p.rounds ? (int64_t)2 * B * (sizeof(State) + 8 * p.tiles) : 0;
     return p;
 }
