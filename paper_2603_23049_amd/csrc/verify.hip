@@ -138,7 +138,9 @@ __device__ __forceinline__ void walk(const VerifyArgs &a, const Seq &s, State &s
                 st.fresh = 0;
             } else if (a.draft) {
                 st.a += st.Z;
-                st.need = kNextZ;
+                // Behind the last child the walk ends here: the sum is the draw's, not a test's.
+                const bool ends = (children & (children - 1)) == 0 && c0 + 64 >= s.n;
+                st.need = ends ? kSum : kNextZ;
                 return;
             } else {
                 st.Z -= w;
