@@ -305,15 +305,15 @@ __global__ __launch_bounds__(kRoundThreads) void verify_round_kernel(const Verif
     __shared__ State sh;
     const int tid = threadIdx.x, b = blockIdx.y;
     const Seq s = sequence(a, b);
+    State st;                                    // (read beside the lengths, whatever it is for an empty sequence)
+    if (round > 0) st = a.states[(int64_t)((round - 1) & 1) * a.B + b];
     if (s.n == 0) return;
     const bool lead = blockIdx.x == 0;
     if (tid < 64) {
-        State st;
         if (round == 0) {
             st = start(s, lead);
             walk(a, s, st, lead);
         } else {
-            st = a.states[(int64_t)((round - 1) & 1) * a.B + b];
             if (st.need == kNextZ) {
                 st.Z = add_tiles(a.sums + ((int64_t)st.buf * a.B + b) * a.tiles, a.tiles);
                 st.fresh = 1;
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(kRoundThreads) void verify_round_kernel(const Verif
         }
     }
     __syncthreads();
-    const State st = sh;
+    st = sh;
     if (st.need == kNothing) return;
     tile_sums<false>(a, row_of(a, s, st), kRoundWaves * blockIdx.x + (tid >> 6), kRoundWaves * gridDim.x,
               a.sums + ((int64_t)st.buf * a.B + b) * a.tiles);
@@ -412,12 +412,12 @@ __global__ __launch_bounds__(kFinalThreads) void verify_final_kernel(const Verif
     const float u0 = s.n > 0 ? s.uniforms[0] : 0.f;
     State st;
     if (wave == 0) {
+        // (state and, with one round, sums are read beside the lengths, whatever they are for an empty sequence)
+        if (a.rounds > 0) st = a.states[(int64_t)((a.rounds - 1) & 1) * a.B + b];
         if (a.rounds == 0 || s.n == 0) {
             st = start(s, true);
             walk(a, s, st, true);
         } else {
-            st = a.states[(int64_t)((a.rounds - 1) & 1) * a.B + b];
-            // (with one round the sums are read beside the state, not behind it)
             const double *from = a.sums + ((int64_t)(a.rounds == 1 ? 0 : st.buf) * a.B + b) * a.tiles;
             for (int32_t t = lane; t < a.tiles; t += 64) sums[t] = from[t];
             if (st.need == kNextZ) {
