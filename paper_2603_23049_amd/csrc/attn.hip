@@ -198,6 +198,7 @@ __device__ __forceinline__ void wait_vmem_keep()
 constexpr int kMaxMapSeqs = 128;
 struct AttnWorkMap {
     int32_t n_seq;                      // slots in use (sequences with new tokens)
+    int32_t parts;                      // XCDs that share each kv head, or 1 (locate_item)
     int32_t per_head;                   // work items of all sequences, one kv head
     int32_t chunk;                      // key split: 64-key tiles per item (else unused)
     uint64_t launch;                    // key split: the launch's number (else unused)
@@ -377,7 +378,8 @@ struct Item {
 // XCD-aware order: workgroup L runs on XCD L % 8. The row tiles of one (sequence,
 // kv head), which read the same K/V, go to workgroups of one XCD and share its L2.
 // With Hkv a multiple of 8, XCD x takes kv heads x, x+8, ... of every sequence, so the
-// eight XCDs get equal work.
+// eight XCDs get equal work. With Hkv 1, 2 or 4 and wm.parts = 8 / Hkv, XCDs parts * g .. take equal,
+// consecutive parts of kv head g's items, whose order makes them equal work (launch_group).
 __device__ __forceinline__ Item locate_item(const AttnWorkMap &wm, int32_t Hkv)
 {
     const int lane = threadIdx.x & 63;
@@ -388,6 +390,9 @@ __device__ __forceinline__ Item locate_item(const AttnWorkMap &wm, int32_t Hkv)
         const int hh = i / wm.per_head;
         it.g = x + kXcds * hh;
         it.j = i - hh * wm.per_head;
+    } else if (wm.parts > 1) {
+        it.j = (x & (wm.parts - 1)) * per_xcd + i;
+        it.g = it.j < wm.per_head ? (x * Hkv) / kXcds : Hkv;
     } else {
         const int w = x * per_xcd + i;
         it.g = w / wm.per_head;
@@ -1480,7 +1485,8 @@ int32_t split_chunk(const int32_t *seq, int n, const Seqs &q, int Hkv, int D, in
 // an estimate from the items' mean lost up to 11% against that line in 29 of them, and
 // 30% on two sequences of 2100 new tokens on 90 cached with 28 / 4 heads (103 -> 79 us).
 constexpr int kSimItems = 1024;
-double schedule_time(const int32_t *order, int n, const Seqs &q, int Hkv, int D, int rpw, int n_cu, bool simulate)
+double schedule_time(const int32_t *order, int n, const Seqs &q, int Hkv, int D, int rpw, int n_cu, bool simulate,
+                     int parts)
 {
     const bool rows = rpw > kRowsPerWG, wide = D == 128;
     const float fixed = rows ? (wide ? 10.f : 7.6f) : (wide ? 7.3f : 5.6f);
@@ -1512,12 +1518,13 @@ double schedule_time(const int32_t *order, int n, const Seqs &q, int Hkv, int D,
     if (!simulate) return total * Hkv / n_cu;
     const int n_xcd_cu = std::max(1, std::min(n_cu / kXcds, 64));
     const float idle = wide ? 0.70f : 0.88f;
-    // As locate_item deals them: whole heads to each XCD (then all eight do the same), or
-    // an eighth of all items.
+    // As locate_item deals them: whole heads to each XCD (then all eight do the same), parts of
+    // a head's items to the XCDs that share it, or an eighth of all items.
     const bool whole = Hkv % kXcds == 0;
-    const int all = items * Hkv, per = whole ? all / kXcds : (all + kXcds - 1) / kXcds;
+    const int all = parts > 1 ? items : items * Hkv, xcds = whole ? 1 : parts > 1 ? parts : kXcds;
+    const int per = whole ? all / kXcds : (all + xcds - 1) / xcds;
     float longest = 0.f;
-    for (int x = 0; x < (whole ? 1 : kXcds); ++x) {
+    for (int x = 0; x < xcds; ++x) {
         float end[64] = {};                  // a heap: when each compute unit is free
         float sum = 0.f, last = 0.f;
         int at = (x * per) % items;
@@ -1554,11 +1561,22 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     auto rows_of = [&](int32_t b) { return (int64_t)sq.rows(b) * G; };
     const int sched = g_schedule.load(std::memory_order_relaxed);
     const bool prefer_keys = auto_schedule == PCR_ATTN_SCHEDULE_KEY_HALVES;
+    // XCDs that share a kv head, of sequences of different lengths, take parts of equal numbers of its
+    // items: each sequence goes to the part with the fewest, so that no XCD has all the long ones; the
+    // parts with more come first, so that a part's long ones do not end the XCD before. (In the order
+    // given, with 28 / 4 heads of 128: trees of 1-61 nodes on 0-1901, 37 of them, 43 us, so 34; 23 of 20-300
+    // new tokens on 0-4000 132 and 103. With 8 / 1 heads 30 of 300-900 on 0-4000 261 and 149, 100 of 1-200
+    // on 0-8000 295 and 184. Decode rows stay spread over the row tiles: with more than one in 16 items, or
+    // parts that come out unequal, the order stays; one prompt of 1000 beside 64 decode rows took 63 us
+    // for 60 in parts.)
+    auto tiles_seen = [&](int32_t b) { return key_tiles(sq.last(b, sq.rows(b) - 1)); };
+    const int shared = Hkv < kXcds && kXcds % Hkv == 0 && tiles_seen(seq[0]) > tiles_seen(seq[n - 1]) ? kXcds / Hkv : 1;
     // Slot order: the given order (longest context first), with the decode rows (one
     // new token, one workgroup each, bound by HBM) spread evenly over the prefill
     // tiles (bound by the matrix cores): run back to back they would take every
     // compute unit at once and queue on HBM.
-    auto slot_order = [&](auto tiles_of, int32_t *order) {
+    // Returns the parts of a kv head's items (AttnWorkMap::parts).
+    auto slot_order = [&](auto tiles_of, int32_t *order) -> int {
         int32_t pre[kMaxMapSeqs], dec[kMaxMapSeqs];
         int np = 0, nd = 0;
         int64_t pre_tiles = 0;
@@ -1578,6 +1596,27 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
             for (; di < nd && (int64_t)di * pre_tiles < (int64_t)nd * done; ++di) order[m++] = dec[di];
         }
         for (; di < nd; ++di) order[m++] = dec[di];
+        if (shared == 1 || n <= shared) return 1;
+        int64_t items[kXcds] = {}, all = 0;
+        int part_of[kMaxMapSeqs], given[kMaxMapSeqs];
+        for (int k = 0; k < n; ++k) {
+            const int x = (int)(std::min_element(items, items + shared) - items);
+            items[x] += tiles_of(order[k]);
+            all += tiles_of(order[k]);
+            part_of[k] = x;
+            given[k] = order[k];
+        }
+        if (nd > 0 && np > 0 &&
+            (16 * nd > all || *std::max_element(items, items + shared) * shared > all + all / 8 + shared))
+            return 1;
+        m = 0;
+        for (int i = 0; i < shared; ++i) {
+            const int x = (int)(std::max_element(items, items + shared) - items);
+            items[x] = -1;
+            for (int k = 0; k < n; ++k)
+                if (part_of[k] == x) order[m++] = given[k];
+        }
+        return shared;
     };
 
     // More key-halves items than compute units: row halves from two of their items per
@@ -1589,7 +1628,9 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     // gets row halves only if they are estimated so and all fit the compute units at once.
     // Against the line alone (32 query / 8 kv heads of 128): 64 sequences of 32 new tokens on
     // 3000 cached 200 -> 154 us (key halves), 16 of 128 on 4096 142 -> 129 (row halves), one of
-    // 1280 on 8192 199 -> 180.
+    // 1280 on 8192 199 -> 180. Where XCDs share a head and row halves of 128 dims end in one round,
+    // these take 5% less than estimated against key halves (mean of 45 ragged batches), and are
+    // taken up to an estimate 2% above (16 of 100-700 on 0-8000, 8 / 1 heads: 133 us, key halves 142).
     bool rows = sched == PCR_ATTN_SCHEDULE_ROW_HALVES;
     if (sched == PCR_ATTN_SCHEDULE_AUTO) {
         int64_t tiles = 0, tiles2 = 0;   // row tiles of 128 and of 256 rows, all kv heads
@@ -1601,13 +1642,16 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
         tiles2 *= Hkv;
         if (tiles > n_cu && (!prefer_keys || tiles2 <= n_cu)) {
             const bool simulate = tiles <= std::min(4 * n_cu, kSimItems);
+            int parts = 1;                   // with row halves, in the end
             auto time_of = [&](int rpw) {
                 int32_t order[kMaxMapSeqs];
-                slot_order([&](int32_t b) { return (rows_of(b) + rpw - 1) / rpw; }, order);
-                return schedule_time(order, n, sq, Hkv, pool.head_dim, rpw, n_cu, simulate);
+                parts = slot_order([&](int32_t b) { return (rows_of(b) + rpw - 1) / rpw; }, order);
+                return schedule_time(order, n, sq, Hkv, pool.head_dim, rpw, n_cu, simulate, parts);
             };
             const bool line = tiles2 >= 2 * (int64_t)n_cu;
-            rows = time_of(2 * kRowsPerWG) < (line ? 1.04 : 0.96) * time_of(kRowsPerWG);
+            const double keys_time = time_of(kRowsPerWG), rows_time = time_of(2 * kRowsPerWG);
+            const bool round = pool.head_dim == 128 && parts > 1 && tiles2 <= n_cu && !prefer_keys;
+            rows = rows_time < (line ? 1.04 : round ? 1.02 : 0.96) * keys_time;
         }
     }
     const int64_t rpw = rows ? 2 * kRowsPerWG : kRowsPerWG;
@@ -1622,7 +1666,7 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     };
 
     AttnWorkMap wm;
-    slot_order(tiles_of, wm.seq);
+    wm.parts = slot_order(tiles_of, wm.seq);
     int32_t cum = 0;
     for (int k = 0; k < n; ++k) {
         const int32_t b = wm.seq[k];
