@@ -15,8 +15,8 @@
 // walk itself is a few dependent loads) and then sum their tiles of the row it needs. The last
 // launch, one workgroup per sequence, ends the walk (with passes of its own where a walk needs more
 // rounds than were launched) and draws: the tile sums lead to the tile, which is read once more. (64 chains of
-// 4 over 128000 tokens: a round 13.5 us, of which the rows' 57 MB take 9 and the walk before them four
-// dependent loads; the draw 8.3, dependent loads too.)
+// 4 over 128000 tokens: a round 12.6 us, of which the rows' 57 MB take 9 and the walk before them four
+// dependent loads; the draw 7.0, dependent loads too.)
 #include <algorithm>
 
 #include "pcr_internal.h"
@@ -480,7 +480,7 @@ struct Plan {
 // Rounds: none where one workgroup sums a row in a few steps (up to 8 tiles; one sequence of 32 took 12.5 us
 // without and 11.7 with a round), or where the sequences alone fill the device. One for a draft
 // without probabilities, which needs one sum, and for short drafts: a chain of 4 needs one sum too (64 of 128000
-// tokens: 30.7 us without a round, 22.3 with one, 28.6 with two, each idle one 2.8). Trees refuse more: a pass in
+// tokens: 30.7 us without a round, 22.3 with one (now 20.4), 28.6 with two, each idle one 2.8). Trees refuse more: a pass in
 // the last launch, with one workgroup per sequence, takes about 15 us of 128000 tokens, in a round
 // 5 and less (128 trees of 12: 94 us without, 106, 102, 83, 67 and 75 with one to five); of few tiles a pass
 // takes no more than an idle round.
