@@ -1546,6 +1546,80 @@ double schedule_time(const int32_t *order, int n, const Seqs &q, int Hkv, int D,
     return longest;
 }
 
+// Slot order of a launch: the given order (longest context first), with the decode rows (one
+// new token, one workgroup each, bound by HBM) spread evenly over the prefill
+// tiles (bound by the matrix cores): run back to back they would take every
+// compute unit at once and queue on HBM.
+//
+// XCDs that share a kv head, of sequences of different lengths, take parts of equal numbers of its
+// items: each sequence goes to the part with the fewest, so that no XCD has all the long ones; the
+// parts with more come first, so that a part's long ones do not end the XCD before. (In the order
+// given, with 28 / 4 heads of 128: trees of 1-61 nodes on 0-1901, 37 of them, 43 us, so 34; 23 of 20-300
+// new tokens on 0-4000 132 and 103. With 8 / 1 heads 30 of 300-900 on 0-4000 261 and 149, 100 of 1-200
+// on 0-8000 295 and 184. Decode rows stay spread over the row tiles: with more than one in 16 items, or
+// parts that come out unequal, the order stays; one prompt of 1000 beside 64 decode rows took 63 us
+// for 60 in parts.)
+// Where one sequence holds more items than a part has, the parts come out unequal and an XCD begins the long
+// items of the next part behind the last of this one. Row tiles alone (up to kSimItems) then go in the given
+// order unless parts are estimated to take 2% less. Given order / parts, us: 6 sequences of 16 new tokens on 8000
+// with 900 on 2000 and 2000 on none, 16 / 2 heads of 128 85 / 108 and 32 / 4 110 / 101; 20 of 16 on 8000 with 1600 on none,
+// 32 / 4 heads of 64 77 / 85 and of 128 103 / 111; 30 of 16 on 4000 with 1000 69 / 57.
+//
+// Returns the parts of a kv head's items (AttnWorkMap::parts). rpw: rows of an item, 0 where tiles_of counts
+// the parts of a key split, which all run at once.
+template <class Tiles>
+int slot_order(const int32_t *seq, int n, const Seqs &sq, int Hkv, int D, int rpw, int n_cu, Tiles tiles_of,
+               int32_t *order)
+{
+    int32_t pre[kMaxMapSeqs], dec[kMaxMapSeqs];
+    int np = 0, nd = 0;
+    int64_t pre_tiles = 0;
+    for (int k = 0; k < n; ++k) {
+        if (sq.few(seq[k])) {
+            dec[nd++] = seq[k];
+        } else {
+            pre[np++] = seq[k];
+            pre_tiles += tiles_of(seq[k]);
+        }
+    }
+    int m = 0, di = 0;
+    int64_t done = 0;
+    for (int k = 0; k < np; ++k) {
+        order[m++] = pre[k];
+        done += tiles_of(pre[k]);
+        for (; di < nd && (int64_t)di * pre_tiles < (int64_t)nd * done; ++di) order[m++] = dec[di];
+    }
+    for (; di < nd; ++di) order[m++] = dec[di];
+    auto tiles_seen = [&](int32_t b) { return key_tiles(sq.last(b, sq.rows(b) - 1)); };
+    const int shared = Hkv < kXcds && kXcds % Hkv == 0 && tiles_seen(seq[0]) > tiles_seen(seq[n - 1]) ? kXcds / Hkv : 1;
+    if (n <= shared || shared == 1) return 1;
+    int64_t items[kXcds] = {}, all = 0;
+    int part_of[kMaxMapSeqs], given[kMaxMapSeqs];
+    for (int k = 0; k < n; ++k) {
+        const int x = (int)(std::min_element(items, items + shared) - items);
+        items[x] += tiles_of(order[k]);
+        all += tiles_of(order[k]);
+        part_of[k] = x;
+        given[k] = order[k];
+    }
+    const bool unequal = *std::max_element(items, items + shared) * shared > all + all / 8 + shared;
+    if (nd > 0 && np > 0 && (16 * nd > all || unequal)) return 1;
+    m = 0;
+    for (int i = 0; i < shared; ++i) {
+        const int x = (int)(std::max_element(items, items + shared) - items);
+        items[x] = -1;
+        for (int k = 0; k < n; ++k)
+            if (part_of[k] == x) order[m++] = given[k];
+    }
+    if (unequal && rpw > 0 && all * Hkv <= kSimItems &&
+        schedule_time(order, n, sq, Hkv, D, rpw, n_cu, true, shared) >
+            0.98 * schedule_time(given, n, sq, Hkv, D, rpw, n_cu, true, 1)) {
+        std::copy(given, given + n, order);
+        return 1;
+    }
+    return shared;
+}
+
 // One launch over the sequences seq[0..n) (each with new tokens, n <= kMaxMapSeqs,
 // longest context first): builds the work map, picks the schedule, launches. split_ws: of
 // cross and tree attention, the workspace of a key split; visible, words: of tree attention.
@@ -1561,64 +1635,6 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     auto rows_of = [&](int32_t b) { return (int64_t)sq.rows(b) * G; };
     const int sched = g_schedule.load(std::memory_order_relaxed);
     const bool prefer_keys = auto_schedule == PCR_ATTN_SCHEDULE_KEY_HALVES;
-    // XCDs that share a kv head, of sequences of different lengths, take parts of equal numbers of its
-    // items: each sequence goes to the part with the fewest, so that no XCD has all the long ones; the
-    // parts with more come first, so that a part's long ones do not end the XCD before. (In the order
-    // given, with 28 / 4 heads of 128: trees of 1-61 nodes on 0-1901, 37 of them, 43 us, so 34; 23 of 20-300
-    // new tokens on 0-4000 132 and 103. With 8 / 1 heads 30 of 300-900 on 0-4000 261 and 149, 100 of 1-200
-    // on 0-8000 295 and 184. Decode rows stay spread over the row tiles: with more than one in 16 items, or
-    // parts that come out unequal, the order stays; one prompt of 1000 beside 64 decode rows took 63 us
-    // for 60 in parts.)
-    auto tiles_seen = [&](int32_t b) { return key_tiles(sq.last(b, sq.rows(b) - 1)); };
-    const int shared = Hkv < kXcds && kXcds % Hkv == 0 && tiles_seen(seq[0]) > tiles_seen(seq[n - 1]) ? kXcds / Hkv : 1;
-    // Slot order: the given order (longest context first), with the decode rows (one
-    // new token, one workgroup each, bound by HBM) spread evenly over the prefill
-    // tiles (bound by the matrix cores): run back to back they would take every
-    // compute unit at once and queue on HBM.
-    // Returns the parts of a kv head's items (AttnWorkMap::parts).
-    auto slot_order = [&](auto tiles_of, int32_t *order) -> int {
-        int32_t pre[kMaxMapSeqs], dec[kMaxMapSeqs];
-        int np = 0, nd = 0;
-        int64_t pre_tiles = 0;
-        for (int k = 0; k < n; ++k) {
-            if (sq.few(seq[k])) {
-                dec[nd++] = seq[k];
-            } else {
-                pre[np++] = seq[k];
-                pre_tiles += tiles_of(seq[k]);
-            }
-        }
-        int m = 0, di = 0;
-        int64_t done = 0;
-        for (int k = 0; k < np; ++k) {
-            order[m++] = pre[k];
-            done += tiles_of(pre[k]);
-            for (; di < nd && (int64_t)di * pre_tiles < (int64_t)nd * done; ++di) order[m++] = dec[di];
-        }
-        for (; di < nd; ++di) order[m++] = dec[di];
-        if (shared == 1 || n <= shared) return 1;
-        int64_t items[kXcds] = {}, all = 0;
-        int part_of[kMaxMapSeqs], given[kMaxMapSeqs];
-        for (int k = 0; k < n; ++k) {
-            const int x = (int)(std::min_element(items, items + shared) - items);
-            items[x] += tiles_of(order[k]);
-            all += tiles_of(order[k]);
-            part_of[k] = x;
-            given[k] = order[k];
-        }
-        if (nd > 0 && np > 0 &&
-            (16 * nd > all || *std::max_element(items, items + shared) * shared > all + all / 8 + shared))
-            return 1;
-        m = 0;
-        for (int i = 0; i < shared; ++i) {
-            const int x = (int)(std::max_element(items, items + shared) - items);
-            items[x] = -1;
-            for (int k = 0; k < n; ++k)
-                if (part_of[k] == x) order[m++] = given[k];
-        }
-        return shared;
-    };
-
     // More key-halves items than compute units: row halves from two of their items per
     // compute unit on (each then pays its start and end for twice the work), and on either
     // side of that line the other schedule when it is estimated to take 4% less. Key
@@ -1645,7 +1661,8 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
             int parts = 1;                   // with row halves, in the end
             auto time_of = [&](int rpw) {
                 int32_t order[kMaxMapSeqs];
-                parts = slot_order([&](int32_t b) { return (rows_of(b) + rpw - 1) / rpw; }, order);
+                parts = slot_order(seq, n, sq, Hkv, pool.head_dim, rpw, n_cu,
+                                   [&](int32_t b) { return (rows_of(b) + rpw - 1) / rpw; }, order);
                 return schedule_time(order, n, sq, Hkv, pool.head_dim, rpw, n_cu, simulate, parts);
             };
             const bool line = tiles2 >= 2 * (int64_t)n_cu;
@@ -1666,7 +1683,7 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     };
 
     AttnWorkMap wm;
-    wm.parts = slot_order(tiles_of, wm.seq);
+    wm.parts = slot_order(seq, n, sq, Hkv, pool.head_dim, chunk ? 0 : (int)rpw, n_cu, tiles_of, wm.seq);
     int32_t cum = 0;
     for (int k = 0; k < n; ++k) {
         const int32_t b = wm.seq[k];
@@ -1808,6 +1825,15 @@ hipError_t launch_batch(const void *q, const pcr_kv_pool &pool, const int32_t *b
     return hipSuccess;
 }
 }  // namespace
+
+int32_t prefill_attn_parts(const int32_t *seq, int32_t n, const int32_t *prefix_lens, const int32_t *cu_suffix,
+                           int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t rpw, int32_t n_cu)
+{
+    const Seqs sq{prefix_lens, cu_suffix, kCausal, num_q_heads / num_kv_heads};
+    int32_t order[kMaxMapSeqs];
+    return slot_order(seq, n, sq, num_kv_heads, head_dim, rpw, n_cu,
+                      [&](int32_t b) { return ((int64_t)sq.rows(b) * sq.G + rpw - 1) / rpw; }, order);
+}
 
 hipError_t launch_prefix_prefill_attn(const void *q, const pcr_kv_pool &pool,
                                       const int32_t *block_tables, int32_t max_blocks,

@@ -62,6 +62,10 @@ int64_t cross_tiles_workspace_bytes();
 hipError_t launch_cross_tiles(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
                               const int32_t *host_key_lens, const int32_t *host_cu_q, int32_t B, int32_t num_q_heads,
                               int32_t T, float sm_scale, void *out, void *workspace, hipStream_t s, int n_cu);
+// Parts of a kv head's items that the XCDs sharing it take in a launch on row tiles of rpw rows over the sequences
+// seq[0..n), n <= 128, longest context first (slot_order); 1: the given order.
+int32_t prefill_attn_parts(const int32_t *seq, int32_t n, const int32_t *prefix_lens, const int32_t *cu_suffix,
+                           int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t rpw, int32_t n_cu);
 // Tree attention by row tiles (attn.hip), of any number of rows; workspace as for cross attention.
 hipError_t launch_tree_tiles(const void *q, const pcr_kv_pool &pool, const int32_t *block_tables, int32_t max_blocks,
                              const int32_t *host_prefix_lens, const int32_t *host_cu_nodes, int32_t B,
