@@ -626,8 +626,12 @@ pcr_status pcr_tree_attn_workspace_size(int32_t B, int32_t total_nodes, int32_t 
                                         int32_t head_dim, int32_t max_keys, int64_t *bytes);
 
 /*
- * pcr_verify_drafts -- which drafted tokens stay, and the token after them, so that the tokens
- * of a step are distributed as the target's (speculative sampling, over a tree). The walk of
+ * pcr_verify_drafts -- which drafted tokens stay, and the token after them (speculative sampling, over a
+ * tree). The tokens of a step are distributed as the target's if, with draft_probs, the drafted children of
+ * a node u were drawn from q_u independently of each other (with replacement: two may be the same token);
+ * children drawn without replacement, or the best of q_u, are not so, and in general neither are the tokens. Without
+ * draft_probs they are, however the children were chosen, provided that what was chosen does not
+ * depend on the uniforms. The walk of
  * sequence b starts on node u = 0. With p_u the target's distribution behind node u, q_u the one
  * that u's drafted children were drawn from, and a = 0, Z = 1, the children of u (nodes i >= 1 with
  * parents[i] = u) are tried in their order: with x = tokens[i] and w = max(p_u(x) - a q_u(x), 0)
@@ -641,8 +645,10 @@ pcr_status pcr_tree_attn_workspace_size(int32_t B, int32_t total_nodes, int32_t 
  * none). If S = 0, r = p_u takes its place. The walk ends too once path_cap nodes stay.
  *   cu_nodes[B+1], parents[T], tokens[T], prefix_lens[B]   device int32, read; T as for
  *                  pcr_draft_tree. A token outside [0, vocab) never stays and refuses nothing.
- *   target_probs   device fp32: row t (node t's) at t * target_stride elements, vocab of them;
- *   draft_probs    likewise, or NULL; row t is read only where a child of node t is tried
+ *   target_probs   device fp32: row t (node t's) at t * target_stride elements, vocab of them
+ *   draft_probs    likewise, or NULL. Row t may be read wherever node t has a child with a token in
+ *                  [0, vocab), whether or not the walk comes there, and is not read elsewhere; what
+ *                  rows of nodes hold that the walk does not come to changes nothing
  *   uniforms       device fp32 [T], in [0, 1)
  *   path           device int32 [B][path_cap], written: the nodes that stay, node 0 first, -1 after
  *   accepted_lens  device int32 [B]: how many (1 + the drafted tokens that stay; 0 if n_b = 0)

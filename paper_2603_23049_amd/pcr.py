@@ -756,7 +756,8 @@ def verify_drafts(cu_nodes, parents, tokens, target_probs, draft_probs, uniforms
                   next_tokens, context_lens, workspace=None, stream=None):
     """pcr_verify_drafts: cu_nodes [B+1], parents and tokens [T], prefix_lens, accepted_lens,
     next_tokens and context_lens [B], path [B][path_cap] int32; target_probs and draft_probs (or
-    None) [T][vocab] float32 with any row stride, uniforms [T] float32; device tensors. context_lens may
+    None) [T][vocab] float32 with any row stride, uniforms [T] float32; device tensors. With draft_probs a
+    node's children must be drawn from its row independently, with replacement. context_lens may
     be prefix_lens. Without a workspace one of the needed size is allocated as decode_attn does."""
     B, T, gpu = prefix_lens.shape[0], parents.shape[0], _current_gpu()
     if target_probs.dim() != 2 or path.dim() != 2:
