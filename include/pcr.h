@@ -688,9 +688,10 @@ pcr_status pcr_verify_drafts_workspace_size(int32_t B, int32_t T, int32_t vocab,
  *   block_tables   device int32 [B][max_blocks]; the blocks from position p_b on belong to b alone
  *   prefix_lens[B], path[B][path_cap], accepted_lens[B]   device int32 (pcr_verify_drafts);
  *                  an accepted_lens beyond path_cap counts as path_cap
- * A path is strictly ascending from 0 or above, as every way down a tree is. The moves of a
- * sequence end before the first entry that is not, whose position is past the table's row, or whose
- * block is outside the pool; none are made for a negative prefix.
+ * A path is strictly ascending from 0 or above, as every way down a tree is. An entry path[b][i] = i is in
+ * its place: nothing moves, and its slot is not looked at. The moves of a sequence end before the first
+ * entry that does not ascend, or that moves from or to a position past the table's row or in a block
+ * outside the pool; none are made for a negative prefix.
  * Errors: as pcr_append_kv for each pool; PCR_ERR_INVALID_ARG for negative counts, pools of
  * different shapes or that overlap, max_blocks or path_cap < 1, NULL arrays; PCR_ERR_UNSUPPORTED beyond
  * 256 layers, 65535 sequences or 2^27 blocks. n_layers = 0 or B = 0 is a no-op.
