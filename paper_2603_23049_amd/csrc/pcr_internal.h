@@ -145,6 +145,13 @@ constexpr int32_t kMaxTreeSeqs = 1 << 21;    // a workgroup of up to 1024 thread
 constexpr int32_t kMaxTreeNodes = 1 << 27;
 constexpr int32_t kMaxVocab = 1 << 30;
 constexpr int64_t kMaxRowStride = (int64_t)1 << 32;   // elements; times the rows, below 2^62 bytes
+// How a verification of B sequences with T rows in all is cut up (verify.hip).
+struct VerifyPlan {
+    int32_t tiles, pieces;   // of a row, and of a tile
+    int32_t rounds, wgs;     // launches before the last one, and their workgroups per sequence
+    int64_t bytes;           // of workspace
+};
+VerifyPlan verify_plan(int32_t B, int32_t T, int32_t V, bool drawn);
 // Size of the allocation-free decode entry point's per-device scratch (decode.hip),
 // and its device address on the current device (taken with hipGetSymbolAddress on the
 // first call per device, then reused).

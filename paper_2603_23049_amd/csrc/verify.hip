@@ -471,22 +471,20 @@ __global__ __launch_bounds__(kFinalThreads) void verify_final_kernel(const Verif
     if (lane == 0) a.next_tokens[b] = token;
 }
 
-// How a call is cut up.
 constexpr int32_t kRoundSeqs = 1024;      // sequences up to which there are rounds
-struct Plan {
-    int32_t tiles, pieces, rounds, wgs;
-    int64_t bytes;                        // of workspace
-};
-// Rounds: none where one workgroup sums a row in a few steps (up to 8 tiles; one sequence of 32 took 12.5 us
+
+}  // namespace
+
+// How a call is cut up. Rounds: none where one workgroup sums a row in a few steps (up to 8 tiles; one sequence of 32 took 12.5 us
 // without and 11.7 with a round), or where the sequences alone fill the device. One for a draft
 // without probabilities, which needs one sum, and for short drafts: a chain of 4 needs one sum too (64 of 128000
 // tokens: 30.7 us without a round, 22.3 with one (now 20.4), 28.6 with two, each idle one 2.8). Trees refuse more: a pass in
 // the last launch, with one workgroup per sequence, takes about 15 us of 128000 tokens, in a round
 // 5 and less (128 trees of 12: 94 us without, 106, 102, 83, 67 and 75 with one to five); of few tiles a pass
 // takes no more than an idle round.
-Plan make_plan(int32_t B, int32_t T, int32_t V, bool drawn)
+VerifyPlan verify_plan(int32_t B, int32_t T, int32_t V, bool drawn)
 {
-    Plan p{};
+    VerifyPlan p{};
     p.pieces = (int32_t)(((int64_t)V + (int64_t)kPiece * kMaxTiles - 1) / ((int64_t)kPiece * kMaxTiles));
     const int64_t size = (int64_t)p.pieces * kPiece;
     p.tiles = (int32_t)((V + size - 1) / size);
@@ -501,7 +499,6 @@ Plan make_plan(int32_t B, int32_t T, int32_t V, bool drawn)
     return p;
 }
 
-}  // namespace
 }  // namespace pcr
 
 using namespace pcr;
@@ -515,7 +512,7 @@ pcr_status pcr_verify_drafts_workspace_size(int32_t B, int32_t T, int32_t vocab,
     if (!bytes) return fail(PCR_ERR_INVALID_ARG, "%s: bytes is NULL", who);
     *bytes = 0;
     if (B < 0 || T < 0 || vocab < 1) return fail(PCR_ERR_INVALID_ARG, "%s: negative B or T, or vocab < 1", who);
-    if (B > 0) *bytes = make_plan(std::min(B, kRoundSeqs), T, vocab, true).bytes;
+    if (B > 0) *bytes = verify_plan(std::min(B, kRoundSeqs), T, vocab, true).bytes;
     return PCR_OK;
 }
 
@@ -540,7 +537,7 @@ pcr_status pcr_verify_drafts(int32_t B, const int32_t *cu_nodes, const int32_t *
     if (!cu_nodes || !prefix_lens || !path || !accepted_lens || !next_tokens || !context_lens ||
         (T > 0 && (!parents || !tokens || !target_probs || !uniforms)))
         return fail(PCR_ERR_INVALID_ARG, "%s: NULL argument", who);
-    const Plan plan = make_plan(B, T, vocab, draft_probs != nullptr);
+    const VerifyPlan plan = verify_plan(B, T, vocab, draft_probs != nullptr);
     const pcr_status st = check_workspace(plan.bytes, workspace, workspace_bytes, who);
     if (st) return st;
     State *states = static_cast<State *>(workspace);
