@@ -117,6 +117,9 @@ struct RowsCost {
 };
 CrossRowsPlan rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t n_cu,
                         const RowsCost &cost);
+// Tree attention's (tree.hip), of up to cols packed rows a sequence.
+CrossRowsPlan tree_rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t cols,
+                             int32_t n_cu);
 // Most slots of any plan (none has more than its steps, either).
 int64_t cross_rows_max_slots(int32_t head_dim, int32_t n_cu);
 // The run of an even cut that holds step x.

@@ -26,6 +26,19 @@ constexpr int kMaxRows = kTreeMaxCols;
 int64_t key_steps(int64_t n) { return (n + 31) / 32; }
 
 }  // namespace
+
+// Constants for two sets of registers where cross attention has three (one sequence, four nodes of 32 / 8
+// heads of 128 over 500 and 2000 keys: whole pairs 13.5 and 26.9 us, eight parts 13.8 and 15.2; 8 / 8 heads of
+// 64 over 1000 and 4000: 11.5 and 24.1, 14.3 and 13.9). Two tiles of columns leave twice the partial
+// results (64 ragged sequences of up to 4096 keys, eight nodes of 32 / 8 heads: even runs 142 us, whole pairs 133). Eight waves of a pair, as cross
+// attention has with 64 dims, merge longer than they save: 8 / 8 heads over 2000 keys 16.4 us, four 15.2.
+CrossRowsPlan tree_rows_plan(int64_t steps, int64_t pairs, int64_t longest, int32_t head_dim, int32_t cols,
+                             int32_t n_cu)
+{
+    return rows_plan(steps, pairs, longest, head_dim, n_cu,
+                     {head_dim == 128 ? 0.29f : 0.15f, 11.f, cols > 16 ? 1.25f : 1.f, 4});
+}
+
 }  // namespace pcr
 
 using namespace pcr;
@@ -120,13 +133,8 @@ pcr_status pcr_tree_attn(const void *q, const pcr_kv_pool *pool, const int32_t *
     hipError_t e;
     if (most <= kMaxRows) {
         if (steps > INT32_MAX) return fail(PCR_ERR_UNSUPPORTED, "%s: batch too large", who);
-        // Constants for two sets of registers where cross attention has three (one sequence, four nodes of 32 / 8
-        // heads of 128 over 500 and 2000 keys: whole pairs 13.5 and 26.9 us, eight parts 13.8 and 15.2; 8 / 8 heads of
-        // 64 over 1000 and 4000: 11.5 and 24.1, 14.3 and 13.9). Two tiles of columns leave twice the partial
-        // results (64 ragged sequences of up to 4096 keys, eight nodes of 32 / 8 heads: even runs 142 us, whole pairs 133). Eight waves of a pair, as cross
-        // attention has with 64 dims, merge longer than they save: 8 / 8 heads over 2000 keys 16.4 us, four 15.2.
-        const CrossRowsPlan plan = rows_plan(steps, (int64_t)B * pool->num_kv_heads, longest, D, n_cu,
-                                             {D == 128 ? 0.29f : 0.15f, 11.f, most > 16 ? 1.25f : 1.f, 4});
+        const CrossRowsPlan plan =
+            tree_rows_plan(steps, (int64_t)B * pool->num_kv_heads, longest, D, (int32_t)most, n_cu);
         bool cut = plan.parts > 1;          // some (sequence, kv head) lies in two runs
         int64_t x = 0;
         for (int32_t b = 0; b < B && !cut && !plan.parts; ++b) {
