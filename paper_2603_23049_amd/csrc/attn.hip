@@ -1553,17 +1553,17 @@ double schedule_time(const int32_t *order, int n, const Seqs &q, int Hkv, int D,
 //
 // XCDs that share a kv head, of sequences of different lengths, take parts of equal numbers of its
 // items: each sequence goes to the part with the fewest, so that no XCD has all the long ones; the
-// parts with more come first, so that a part's long ones do not end the XCD before. (In the order
-// given, with 28 / 4 heads of 128: trees of 1-61 nodes on 0-1901, 37 of them, 43 us, so 34; 23 of 20-300
-// new tokens on 0-4000 132 and 103. With 8 / 1 heads 30 of 300-900 on 0-4000 261 and 149, 100 of 1-200
-// on 0-8000 295 and 184. Decode rows stay spread over the row tiles: with more than one in 16 items, or
-// parts that come out unequal, the order stays; one prompt of 1000 beside 64 decode rows took 63 us
-// for 60 in parts.)
+// parts with more come first, so that a part's long ones do not end the XCD before. Given order / parts, us: with
+// 28 / 4 heads of 128 37 trees of 1-61 nodes on 0-1901 43.5 / 31.9, 23 of 20-300 new tokens on 0-4000
+// 133 / 102; with 8 / 1 heads 30 of 300-900 on 0-4000 305 / 211, 100 of 1-200 on 0-8000 281 / 186.
 // Where one sequence holds more items than a part has, the parts come out unequal and an XCD begins the long
 // items of the next part behind the last of this one. Row tiles alone (up to kSimItems) then go in the given
-// order unless parts are estimated to take 2% less. Given order / parts, us: 6 sequences of 16 new tokens on 8000
-// with 900 on 2000 and 2000 on none, 16 / 2 heads of 128 85 / 108 and 32 / 4 110 / 101; 20 of 16 on 8000 with 1600 on none,
-// 32 / 4 heads of 64 77 / 85 and of 128 103 / 111; 30 of 16 on 4000 with 1000 69 / 57.
+// order unless parts are estimated to take 2% less: 6 sequences of 16 new tokens on 8000 with 900 on 2000 and 2000 on
+// none, 16 / 2 heads of 128 85 / 108; 20 of 16 on 8000 with 1600 on none, 32 / 4 heads of 64 77 / 85 and of 128
+// 103 / 111; 30 of 16 on 4000 with 1000 on none 69 / 57 (taken).
+// Beside decode rows the order stays where these are more than one item in 16 or the parts unequal. Parts
+// cost nothing there and often gain (64 decode rows on 500-4000 with 1000 new tokens on 2000, 28 / 4 heads
+// of 128: 80 / 64; with 1000 on none 8 / 1 heads 24.6 / 25.1): the line is cautious.
 //
 // Returns the parts of a kv head's items (AttnWorkMap::parts). rpw: rows of an item, 0 where tiles_of counts
 // the parts of a key split, which all run at once.
@@ -1645,8 +1645,8 @@ hipError_t launch_group(const int32_t *seq, int n, const u16 *qq, const pcr_kv_p
     // Against the line alone (32 query / 8 kv heads of 128): 64 sequences of 32 new tokens on
     // 3000 cached 200 -> 154 us (key halves), 16 of 128 on 4096 142 -> 129 (row halves), one of
     // 1280 on 8192 199 -> 180. Where XCDs share a head and row halves of 128 dims end in one round,
-    // these take 5% less than estimated against key halves (mean of 45 ragged batches), and are
-    // taken up to an estimate 2% above (16 of 100-700 on 0-8000, 8 / 1 heads: 133 us, key halves 142).
+    // they are taken up to an estimate 2% above: of 45 ragged batches three were 3-4% shorter for it (43 of 1-300
+    // on 0-8000, 7 / 1 heads: 166 us, key halves 172) and one 2% longer (16 / 2 heads, 39.6 and 38.9).
     bool rows = sched == PCR_ATTN_SCHEDULE_ROW_HALVES;
     if (sched == PCR_ATTN_SCHEDULE_AUTO) {
         int64_t tiles = 0, tiles2 = 0;   // row tiles of 128 and of 256 rows, all kv heads

@@ -15,8 +15,8 @@
 // walk itself is a few dependent loads) and then sum their tiles of the row it needs. The last
 // launch, one workgroup per sequence, ends the walk (with passes of its own where a walk needs more
 // rounds than were launched) and draws: the tile sums lead to the tile, which is read once more. (64 chains of
-// 4 over 128000 tokens: a round 12.6 us, of which the rows' 57 MB take 9 and the walk before them four
-// dependent loads; the draw 7.0, dependent loads too.)
+// 4 over 128000 tokens: a round 13.0 us, of which the rows' 57 MB take 9 and the walk before them four
+// dependent loads; the draw 7.4, dependent loads too.)
 #include <algorithm>
 
 #include "pcr_internal.h"
@@ -475,13 +475,22 @@ constexpr int32_t kRoundSeqs = 1024;      // sequences up to which there are rou
 
 }  // namespace
 
-// How a call is cut up. Rounds: none where one workgroup sums a row in a few steps (up to 8 tiles; one sequence of 32 took 12.5 us
-// without and 11.7 with a round), or where the sequences alone fill the device. One for a draft
-// without probabilities, which needs one sum, and for short drafts: a chain of 4 needs one sum too (64 of 128000
-// tokens: 30.7 us without a round, 22.3 with one (now 20.4), 28.6 with two, each idle one 2.8). Trees refuse more: a pass in
-// the last launch, with one workgroup per sequence, takes about 15 us of 128000 tokens, in a round
-// 5 and less (128 trees of 12: 94 us without, 106, 102, 83, 67 and 75 with one to five); of few tiles a pass
-// takes no more than an idle round.
+// How a call is cut up. A round, idle, costs 2 us among other launches. A pass over 128000 tokens takes about 15 us in
+// the last launch, with one workgroup a sequence, and 5 or less in a round. With 0, 1, 2 and 4 rounds, us:
+//   chains of 4, 128000 tokens, 64 of them     28.7  20.5  22.4  26.3      8 of them  25.7  12.4  14.3  18.9
+//   one chain of 5, 32001 tokens               12.0  11.4  14.3  19.4
+//   64 chains of 8, 128000 tokens              29.8  22.1  24.1  27.9      of 16      30.5  23.7  25.4  29.6
+//   trees of 13 nodes, 128 of 128000 tokens    91.5  93.6  86.3  64.2      (three 75.9, five 66.7)
+//   64 trees of 9 nodes, 128000 tokens         73.3  66.2  55.4  40.6      of 5       73.6  65.5  54.2  39.3
+//   64 trees of 13, 8192 tokens                17.9  21.2  23.4            9217       20.4  23.2  25.0
+//                   16384                      20.5  23.2  24.4  27.4      40960      31.4  32.3  30.6  30.4
+//                   49152                      39.2  38.6  36.2  31.7
+//   48 trees, no probabilities, 50001 tokens   18.2  15.0  17.0  21.3
+//   512 trees of 4, 32000 tokens               45.6  48.7  46.5            1024       81.8  85.8  83.6
+// So none up to 8 tiles, and where the sequences alone fill the device; one for a draft without probabilities (it
+// needs one sum), below 48 tiles, and for few nodes; four for many, two between. What a walk needs
+// follows from its refusals, so from siblings, which the host does not know and the mean number of nodes stands
+// for: long chains pay idle rounds, and small trees take passes in the last launch.
 VerifyPlan verify_plan(int32_t B, int32_t T, int32_t V, bool drawn)
 {
     VerifyPlan p{};
@@ -491,8 +500,8 @@ VerifyPlan verify_plan(int32_t B, int32_t T, int32_t V, bool drawn)
     const int64_t nodes = ((int64_t)T + std::max(B, 1) - 1) / std::max(B, 1);
     p.rounds = p.tiles <= 8 || B > kRoundSeqs ? 0 : !drawn || nodes <= 5 || p.tiles < 48 ? 1 : nodes <= 9 ? 2 : 4;
     // Two tiles a wave where the sequences fill the device that way, one where they are fewer, more where they
-    // are many (64 chains of 4, 128000 tokens: one tile a wave 24.7 us, two 22.7; 128 trees of 12: 67.6 and 68.1,
-    // four 74.8).
+    // are many (one, two and four, us: 64 chains of 4 of 128000 tokens 22.5, 20.4, 21.8; 16 of them 14.0, 15.4, 19.0; 256 of
+    // 50000 29.3, 28.6, 27.3; 128 trees of 13 nodes of 128000 91.4, 91.5, 101).
     const int64_t seqs = std::max(B, 1), one = (p.tiles + kRoundWaves - 1) / kRoundWaves, two = (one + 1) / 2;
     p.wgs = (int32_t)std::max<int64_t>(1, std::min(one, std::max(1024 / seqs, std::min(two, 4096 / seqs))));
     p.bytes = p.rounds ? (int64_t)2 * B * (sizeof(State) + 8 * p.tiles) : 0;
