@@ -379,7 +379,7 @@ struct Item {
 // kv head), which read the same K/V, go to workgroups of one XCD and share its L2.
 // With Hkv a multiple of 8, XCD x takes kv heads x, x+8, ... of every sequence, so the
 // eight XCDs get equal work. With Hkv 1, 2 or 4 and wm.parts = 8 / Hkv, XCDs parts * g .. take equal,
-// consecutive parts of kv head g's items, whose order makes them equal work (launch_group).
+// consecutive parts of kv head g's items, whose order makes them equal work (slot_order).
 __device__ __forceinline__ Item locate_item(const AttnWorkMap &wm, int32_t Hkv)
 {
     const int lane = threadIdx.x & 63;
